@@ -675,6 +675,109 @@ int dgnn_evolve_weights_backward(const float *w0, const float *u_x, const float 
  */
 int dgnn_add(const void *a, const void *b, void *out, int64_t n, int32_t f, dgnn_dtype dt, void *stream);
 
+/*
+ * ---- A temporal layer beside the LSTM (Section "CD-GCN" puts one over the snapshots of a vertex): a short causal convolution
+ * over time and a scan whose recurrence is linear in its state and gated by its input.  The GCN operation's frames go in, projections
+ * between the steps are dgnn_feature_transform, and a series processed in blocks (Section "Gradient Checkpoint") hands the last
+ * frames and the state from block to block, their gradients back.  One timestep (T = 1), its state updated in place, is the step of a
+ * model that follows a running series.
+ *
+ * Both take f channels, a multiple of 16 up to DGNN_MAX_CHANNELS, and sequences of different lengths: lengths [n] int32 or NULL (all T;
+ * values are brought into 0 .. T on the device).  Sequence v then has timesteps 0 .. lengths[v]-1: what lies behind is not looked at, its
+ * outputs and gradients are zero, and states are those after the last timestep there is.  Parameters (taps, bias, a, d, dt_bias) and their
+ * gradients are fp32 whatever dt is and need the alignment of a float only.
+ */
+#define DGNN_MAX_CHANNELS 16384
+#define DGNN_SILU 8u             /* flag of dgnn_causal_conv and its adjoint: silu(a) = a / (1 + exp(-a)) of the result */
+
+/*
+ * Causal convolution over time, one filter per channel: y[t] = act(bias + sum_{j<w} taps[j] x[t-j]), w = 2, 3 or 4.
+ *   x, y [T][n][f]         storage type dt; sums in fp32, rounded once
+ *   taps [w][f], bias [f]  taps[0] belongs to the current frame; bias may be NULL
+ *   x_before [w-1][n][f]   the frames ahead of the series, oldest first, or NULL (zeros)
+ *   x_after [w-1][n][f]    receives the last w-1 frames of (x_before, x), or NULL; may be x_before, and no other input or output
+ *   flags                  DGNN_SILU or 0
+ * Errors: NULL, SHAPE, OVERFLOW (T * n beyond 2^44 too), ALIGN, ALIAS.
+ */
+int dgnn_causal_conv(const void *x, const float *taps, const float *bias, const void *x_before, void *y, void *x_after,
+                     const int32_t *lengths, int64_t T, int64_t n, int32_t f, int32_t w, uint32_t flags, dgnn_dtype dt, void *stream);
+
+/*
+ * Its adjoint.  x, taps, bias, x_before, flags as in the forward call (pre-activations are formed again), g_y = dL/dy,
+ *   dx_after [w-1][n][f]   dL/dx_after, from the block behind, or NULL (zero)
+ *   dx [T][n][f], dx_before [w-1][n][f] or NULL;   dtaps [w][f], dbias [f] (NULL where bias is) fp32: written, or added to with
+ *   accumulate != 0.  Sums over time and sequences have a fixed order (fp32 within a workgroup, 64 bits over the workgroups).
+ *   ws: dgnn_causal_conv_backward_workspace() bytes.  Outputs overlap neither inputs nor each other.
+ */
+int dgnn_causal_conv_backward_workspace(int64_t T, int64_t n, int32_t f, int32_t w, size_t *bytes);
+int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bias, const void *x_before, const void *g_y,
+                              const void *dx_after, void *dx, void *dx_before, float *dtaps, float *dbias, const int32_t *lengths,
+                              int64_t T, int64_t n, int32_t f, int32_t w, uint32_t flags, int32_t accumulate, dgnn_dtype dt,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Selective state-space scan, `states` = N states per channel, 8, 16 or 32:
+ *     s[t] = softplus(delta[t] + dt_bias),   h[t][c][k] = exp(s[t][c] a[c][k]) h[t-1][c][k] + s[t][c] x[t][c] B[t][k],
+ *     y[t][c] = (sum_k C[t][k] h[t][c][k] + d[c] x[t][c]) silu(z[t][c]).
+ *   x, delta, y [T][n][f]        storage type dt
+ *   bc [T][n][2 N]               B | C of a sequence's timestep, which its channels share: one product of dgnn_feature_transform
+ *   z [T][n][f]                  or NULL (no gate)
+ *   a [f][N]; d [f], dt_bias [f] or NULL (zero)
+ *   h_before [n][f][N] fp32      the state ahead of the series, or NULL (zero)
+ *   h_after [n][f][N] fp32       receives the last state, or NULL; may be h_before
+ *   checkpoints                  NULL, or fp32 of dgnn_selective_scan_checkpoints() bytes: the state ahead of every 16th timestep,
+ *                                which is what the adjoint needs of the forward pass
+ *   ws                           dgnn_selective_scan_workspace() bytes, 16-byte aligned
+ * States, step sizes and sums are fp32, y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose
+ * states are joined afterwards: the same sums in another order.  Results repeat bit for bit.
+ * Errors: NULL, SHAPE, OVERFLOW (T * n beyond 2^44 too), ALIGN, ALIAS, CAPACITY.
+ */
+int dgnn_selective_scan_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
+int dgnn_selective_scan_checkpoints(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
+int dgnn_selective_scan(const void *x, const void *delta, const void *bc, const void *z, const float *a, const float *d,
+                        const float *dt_bias, const float *h_before, void *y, float *h_after, float *checkpoints,
+                        const int32_t *lengths, int64_t T, int64_t n, int32_t f, int32_t states, dgnn_dtype dt, void *ws,
+                        size_t ws_bytes, void *stream);
+
+/*
+ * Its adjoint.  Inputs as in the forward call, checkpoints as it left them (h_before is their first), g_y = dL/dy,
+ *   dh_after [n][f][N] fp32      dL/dh_after, from the block behind, or NULL (zero)
+ *   dx, ddelta [T][n][f], dbc [T][n][2 N], dz [T][n][f] (NULL where z is)
+ *   da [f][N], dd [f], ddt_bias [f] (NULL where d, dt_bias are) fp32: written, or added to with accumulate != 0
+ *   dh_before [n][f][N] fp32 or NULL
+ * Sums over channels are fp32, those over time and sequences fp32 over 16 timesteps and 64 bits beyond, all in a fixed order.
+ *   ws: dgnn_selective_scan_backward_workspace() bytes.  Outputs overlap neither inputs nor each other.
+ */
+int dgnn_selective_scan_backward_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
+int dgnn_selective_scan_backward(const void *x, const void *delta, const void *bc, const void *z, const float *a, const float *d,
+                                 const float *dt_bias, const float *checkpoints, const void *g_y, const float *dh_after, void *dx,
+                                 void *ddelta, void *dbc, void *dz, float *da, float *dd, float *ddt_bias, float *dh_before,
+                                 const int32_t *lengths, int64_t T, int64_t n, int32_t f, int32_t states, int32_t accumulate,
+                                 dgnn_dtype dt, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * ---- Between the gradients of a block (Section "Gradient Checkpoint") and the update of the weights: the norm over all of them, and
+ * the gradients scaled so that it is at most max_norm.  One gradient of the set: `count` elements (0 is allowed) of type dt at any
+ * address that its elements may have; out may be g.
+ */
+typedef struct {
+    const void *g;
+    void *out;
+    int64_t count;
+    int64_t dt;                  /* a dgnn_dtype */
+} dgnn_grad_item;
+
+/*
+ * norm[0] (DEVICE fp32) = sqrt(sum of g^2 over all items);  dgnn_grad_clip: out = g * min(1, max_norm / (norm + 1e-6)), rounded once.
+ * A norm that is no finite number leaves the gradients as they are (out = g): the caller finds it in norm[0].  Squares and sums are
+ * in 64 bits, in a fixed order.  What is written overlaps nothing else, but out may be exactly its own g.  items: HOST array, read before
+ * the call returns (dgnn_grad_norm does not look at out).  ws: dgnn_grad_clip_workspace(count) bytes, 16-byte aligned.
+ * Errors: NULL, SHAPE (count <= 0, max_norm not positive), OVERFLOW (an item of more than 2^40 elements), ALIGN, ALIAS, CAPACITY.
+ */
+int dgnn_grad_clip_workspace(int32_t count, size_t *bytes);
+int dgnn_grad_norm(int32_t count, const dgnn_grad_item *items, float *norm, void *ws, size_t ws_bytes, void *stream);
+int dgnn_grad_clip(int32_t count, const dgnn_grad_item *items, double max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,5 +19,9 @@ from .binding import (  # noqa: F401
     # CD-GCN layer and the LSTM over weights
     concat_relu, transform_concat_relu, transform_concat_relu_supported, lstm_cell, lstm_step, lstm_step_supported, lstm_cell_backward, lstm_step_backward,
     lstm_step_backward_supported, lstm_series, lstm_series_backward, lstm_weight_grad, concat_relu_backward, bias_grad, bias_grad_workspace, add,
+    # a temporal layer beside the LSTM
+    causal_conv, causal_conv_backward, causal_conv_backward_workspace, selective_scan, selective_scan_workspace, selective_scan_checkpoints,
+    selective_scan_backward, selective_scan_backward_workspace,
     DGNN_VALIDATE, DGNN_UPDATES_SORTED, DGNN_RELU, DGNN_H_PRESCALED, DGNN_F32, DGNN_BF16,
 )
+from .gradients import Gradients  # noqa: F401

@@ -23,6 +23,8 @@ DGNN_SERIES_STEPS = 31
 DGNN_RELU = 1
 DGNN_H_PRESCALED = 2
 DGNN_W_TRANSPOSED = 4
+DGNN_SILU = 8
+DGNN_MAX_CHANNELS = 16384
 
 EXPORTS = (
     "dgnn_strerror", "dgnn_csr_validate", "dgnn_csr_dinv", "dgnn_delta_h2d", "dgnn_delta_rebuild_workspace",
@@ -34,6 +36,9 @@ EXPORTS = (
     "dgnn_lstm_series", "dgnn_lstm_series_backward", "dgnn_lstm_weight_grad_workspace", "dgnn_lstm_weight_grad",
     "dgnn_evolve_weights", "dgnn_evolve_weights_backward_workspace", "dgnn_evolve_weights_backward",
     "dgnn_mproduct_backward", "dgnn_mproduct_block", "dgnn_mproduct_backward_block", "dgnn_mproduct_relu_backward_block", "dgnn_relu_backward", "dgnn_weight_grad_workspace", "dgnn_weight_grad", "dgnn_input_grad",
+    "dgnn_causal_conv", "dgnn_causal_conv_backward_workspace", "dgnn_causal_conv_backward",
+    "dgnn_selective_scan_workspace", "dgnn_selective_scan_checkpoints", "dgnn_selective_scan", "dgnn_selective_scan_backward_workspace", "dgnn_selective_scan_backward",
+    "dgnn_grad_clip_workspace", "dgnn_grad_norm", "dgnn_grad_clip",
 )
 
 
@@ -154,6 +159,16 @@ def load_library():
     lib.dgnn_weight_grad_workspace.argtypes = [_i32, _i32, ctypes.POINTER(_sz)]
     lib.dgnn_weight_grad.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _i32, ctypes.c_int, _vp, _sz, _vp]
     lib.dgnn_input_grad.argtypes = [_vp, _i64, _i32, _vp, _i32, _vp, _vp, ctypes.c_int, _vp]
+    lib.dgnn_causal_conv.argtypes = [_vp] * 7 + [_i64, _i64, _i32, _i32, ctypes.c_uint32, ctypes.c_int, _vp]
+    lib.dgnn_causal_conv_backward_workspace.argtypes = [_i64, _i64, _i32, _i32, ctypes.POINTER(_sz)]
+    lib.dgnn_causal_conv_backward.argtypes = [_vp] * 11 + [_i64, _i64, _i32, _i32, ctypes.c_uint32, _i32, ctypes.c_int, _vp, _sz, _vp]
+    for name in ("dgnn_selective_scan_workspace", "dgnn_selective_scan_checkpoints", "dgnn_selective_scan_backward_workspace"):
+        getattr(lib, name).argtypes = [_i64, _i64, _i32, _i32, ctypes.POINTER(_sz)]
+    lib.dgnn_selective_scan.argtypes = [_vp] * 12 + [_i64, _i64, _i32, _i32, ctypes.c_int, _vp, _sz, _vp]
+    lib.dgnn_selective_scan_backward.argtypes = [_vp] * 19 + [_i64, _i64, _i32, _i32, _i32, ctypes.c_int, _vp, _sz, _vp]
+    lib.dgnn_grad_clip_workspace.argtypes = [_i32, ctypes.POINTER(_sz)]
+    lib.dgnn_grad_norm.argtypes = [_i32, _vp, _vp, _vp, _sz, _vp]
+    lib.dgnn_grad_clip.argtypes = [_i32, _vp, ctypes.c_double, _vp, _vp, _sz, _vp]
     for name in EXPORTS:
         if name != "dgnn_strerror":
             getattr(lib, name).restype = ctypes.c_int
@@ -814,6 +829,179 @@ def input_grad(g: torch.Tensor, w: torch.Tensor, dx: torch.Tensor, row_scale: Op
         _need(row_scale, torch.float32, "row_scale")
     _check(load_library().dgnn_input_grad(_ptr(g), n, f_out, _ptr(w), f_in, _ptr(row_scale), _ptr(dx), dt, _stream(g)),
            "dgnn_input_grad")
+
+
+def _frames(name: str, like: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
+    """Tensors (or None) of like's shape, type and device."""
+    for t in tensors:
+        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+            raise ValueError(f"shape, dtype or device mismatch in {name}")
+
+
+def _floats(name: str, where: torch.Tensor, shape, *tensors: Optional[torch.Tensor]) -> None:
+    """Contiguous float32 tensors (or None) of this shape on the device of `where`."""
+    for t in tensors:
+        if t is not None:
+            _need(t, torch.float32, name)
+            if tuple(t.shape) != tuple(shape) or t.device != where.device:
+                raise ValueError(f"{name}: expected shape {tuple(shape)} on {where.device}")
+
+
+def _lengths(lengths: Optional[torch.Tensor], x: torch.Tensor) -> None:
+    if lengths is not None:
+        _need(lengths, torch.int32, "lengths")
+        if tuple(lengths.shape) != (x.shape[1],) or lengths.device != x.device:
+            raise ValueError("lengths must have one entry per sequence")
+
+
+def _call(x: torch.Tensor, fn, name: str, *args) -> None:
+    """fn(*args, stream) on the device of x."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} takes tensors on the GPU")
+    if x.device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream(x))
+    else:
+        with torch.cuda.device(x.device):
+            rc = fn(*args, _stream(x))
+    _check(rc, name)
+
+
+def _workspace(ws: torch.Tensor, x: torch.Tensor) -> Tuple[Optional[int], int]:
+    if ws.device != x.device:
+        raise ValueError("the workspace lies on another device")
+    return _ptr(ws), ws.numel() * ws.element_size()
+
+
+def _conv_args(x, taps, bias, *edges):
+    if x.dim() != 3 or taps.dim() != 2:
+        raise ValueError("causal_conv takes x [T, n, f] and taps [w, f]")
+    (T, n, f), w = x.shape, taps.shape[0]
+    _floats("taps", x, (w, f), taps)
+    _floats("bias", x, (f,), bias)
+    for e in edges:
+        if e is not None and (tuple(e.shape) != (w - 1, n, f) or e.dtype != x.dtype or e.device != x.device):
+            raise ValueError("frames handed over must be [w - 1, n, f] of x's type")
+    return T, n, f, w
+
+
+def causal_conv(x: torch.Tensor, taps: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor, silu: bool = False, x_before: Optional[torch.Tensor] = None,
+                x_after: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None) -> None:
+    """y[t] = act(bias + sum_j taps[j] x[t - j]) per channel, over frames [T, n, f]; taps [w, f] and bias [f] float32.  x_before
+    [w - 1, n, f]: the frames ahead (None: zeros); x_after: receives the last w - 1 frames (may be x_before); lengths [n] int32."""
+    dt = _dtype_code(x)
+    T, n, f, w = _conv_args(x, taps, bias, x_before, x_after)
+    _frames("causal_conv", x, y)
+    _lengths(lengths, x)
+    _call(x, load_library().dgnn_causal_conv, "dgnn_causal_conv", _ptr(x), _ptr(taps), _ptr(bias), _ptr(x_before), _ptr(y), _ptr(x_after), _ptr(lengths), T, n, f, w,
+          DGNN_SILU if silu else 0, dt)
+
+
+def causal_conv_backward_workspace(T: int, n: int, f: int, w: int) -> int:
+    out = _sz(0)
+    _check(load_library().dgnn_causal_conv_backward_workspace(T, n, f, w, ctypes.byref(out)), "dgnn_causal_conv_backward_workspace")
+    return int(out.value)
+
+
+def causal_conv_backward(x: torch.Tensor, taps: torch.Tensor, bias: Optional[torch.Tensor], g_y: torch.Tensor, dx: torch.Tensor, dtaps: torch.Tensor,
+                         dbias: Optional[torch.Tensor], ws: torch.Tensor, silu: bool = False, x_before: Optional[torch.Tensor] = None,
+                         dx_after: Optional[torch.Tensor] = None, dx_before: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                         accumulate: bool = False) -> None:
+    """Gradients of causal_conv; dx_after = dL/dx_after from the block behind, dx_before goes to the block ahead."""
+    dt = _dtype_code(x)
+    T, n, f, w = _conv_args(x, taps, bias, x_before, dx_after, dx_before)
+    _frames("causal_conv_backward", x, g_y, dx)
+    _floats("dtaps", x, (w, f), dtaps)
+    _floats("dbias", x, (f,), dbias)
+    _lengths(lengths, x)
+    _call(x, load_library().dgnn_causal_conv_backward, "dgnn_causal_conv_backward", _ptr(x), _ptr(taps), _ptr(bias), _ptr(x_before), _ptr(g_y), _ptr(dx_after), _ptr(dx),
+          _ptr(dx_before), _ptr(dtaps), _ptr(dbias), _ptr(lengths), T, n, f, w, DGNN_SILU if silu else 0, int(bool(accumulate)), dt, *_workspace(ws, x))
+
+
+def selective_scan_workspace(T: int, n: int, f: int, states: int) -> int:
+    out = _sz(0)
+    _check(load_library().dgnn_selective_scan_workspace(T, n, f, states, ctypes.byref(out)), "dgnn_selective_scan_workspace")
+    return int(out.value)
+
+
+def selective_scan_checkpoints(T: int, n: int, f: int, states: int) -> int:
+    """float32 elements that the forward pass leaves for the backward pass."""
+    out = _sz(0)
+    _check(load_library().dgnn_selective_scan_checkpoints(T, n, f, states, ctypes.byref(out)), "dgnn_selective_scan_checkpoints")
+    return int(out.value) // 4
+
+
+def selective_scan_backward_workspace(T: int, n: int, f: int, states: int) -> int:
+    out = _sz(0)
+    _check(load_library().dgnn_selective_scan_backward_workspace(T, n, f, states, ctypes.byref(out)), "dgnn_selective_scan_backward_workspace")
+    return int(out.value)
+
+
+def _scan_args(name, x, delta, bc, z, a, d, dt_bias, checkpoints, lengths):
+    if x.dim() != 3 or a.dim() != 2:
+        raise ValueError(f"{name} takes x [T, n, f] and a [f, states]")
+    (T, n, f), states = x.shape, a.shape[1]
+    _frames(name, x, delta, z)
+    if tuple(bc.shape) != (T, n, 2 * states) or bc.dtype != x.dtype or bc.device != x.device:
+        raise ValueError("bc must be [T, n, 2 states] of x's type")
+    _floats("a", x, (f, states), a)
+    _floats("d, dt_bias", x, (f,), d, dt_bias)
+    _lengths(lengths, x)
+    if checkpoints is not None:
+        _need(checkpoints, torch.float32, "checkpoints")
+        if checkpoints.device != x.device or checkpoints.numel() < (T + 15) // 16 * n * f * states:
+            raise DgnnError(-3, f"{name} (checkpoints)")
+    return T, n, f, states
+
+
+def selective_scan(x: torch.Tensor, delta: torch.Tensor, bc: torch.Tensor, a: torch.Tensor, y: torch.Tensor, ws: torch.Tensor, z: Optional[torch.Tensor] = None,
+                   d: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None, h_before: Optional[torch.Tensor] = None,
+                   h_after: Optional[torch.Tensor] = None, checkpoints: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None) -> None:
+    """The selective state-space scan over frames [T, n, f] (include/dgnn.h): x, delta, z of one type, bc [T, n, 2 states] = B | C,
+    a [f, states], d, dt_bias [f] float32; states [n, f, states] float32, h_after may be h_before.  checkpoints
+    (selective_scan_checkpoints elements) where selective_scan_backward follows; lengths [n] int32."""
+    dt = _dtype_code(x)
+    T, n, f, states = _scan_args("selective_scan", x, delta, bc, z, a, d, dt_bias, checkpoints, lengths)
+    _frames("selective_scan", x, y)
+    _floats("state", x, (n, f, states), h_before, h_after)
+    _call(x, load_library().dgnn_selective_scan, "dgnn_selective_scan", _ptr(x), _ptr(delta), _ptr(bc), _ptr(z), _ptr(a), _ptr(d), _ptr(dt_bias), _ptr(h_before), _ptr(y),
+          _ptr(h_after), _ptr(checkpoints), _ptr(lengths), T, n, f, states, dt, *_workspace(ws, x))
+
+
+def selective_scan_backward(x: torch.Tensor, delta: torch.Tensor, bc: torch.Tensor, a: torch.Tensor, g_y: torch.Tensor, checkpoints: torch.Tensor, dx: torch.Tensor,
+                            ddelta: torch.Tensor, dbc: torch.Tensor, da: torch.Tensor, ws: torch.Tensor, z: Optional[torch.Tensor] = None,
+                            dz: Optional[torch.Tensor] = None, d: Optional[torch.Tensor] = None, dd: Optional[torch.Tensor] = None,
+                            dt_bias: Optional[torch.Tensor] = None, ddt_bias: Optional[torch.Tensor] = None, dh_after: Optional[torch.Tensor] = None,
+                            dh_before: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None, accumulate: bool = False) -> None:
+    """Gradients of selective_scan, from the checkpoints its forward call left; dh_after = dL/dh_after from the block behind, dh_before
+    goes to the block ahead; da, dd, ddt_bias float32, added to with accumulate."""
+    dt = _dtype_code(x)
+    T, n, f, states = _scan_args("selective_scan_backward", x, delta, bc, z, a, d, dt_bias, checkpoints, lengths)
+    _frames("selective_scan_backward", x, g_y, dx, ddelta, dz)
+    _frames("selective_scan_backward", bc, dbc)
+    _floats("da", x, (f, states), da)
+    _floats("dd, ddt_bias", x, (f,), dd, ddt_bias)
+    _floats("state gradient", x, (n, f, states), dh_after, dh_before)
+    _call(x, load_library().dgnn_selective_scan_backward, "dgnn_selective_scan_backward", _ptr(x), _ptr(delta), _ptr(bc), _ptr(z), _ptr(a), _ptr(d), _ptr(dt_bias),
+          _ptr(checkpoints), _ptr(g_y), _ptr(dh_after), _ptr(dx), _ptr(ddelta), _ptr(dbc), _ptr(dz), _ptr(da), _ptr(dd), _ptr(ddt_bias), _ptr(dh_before), _ptr(lengths),
+          T, n, f, states, int(bool(accumulate)), dt, *_workspace(ws, x))
+
+
+def grad_clip_workspace(count: int) -> int:
+    out = _sz(0)
+    _check(load_library().dgnn_grad_clip_workspace(count, ctypes.byref(out)), "dgnn_grad_clip_workspace")
+    return int(out.value)
+
+
+def grad_norm(count: int, items: int, norm: torch.Tensor, ws: torch.Tensor) -> None:
+    """norm[0] of a table of gradients (gradients.py)."""
+    _floats("norm", ws, (1,), norm)
+    _call(norm, load_library().dgnn_grad_norm, "dgnn_grad_norm", count, items, _ptr(norm), *_workspace(ws, norm))
+
+
+def grad_clip(count: int, items: int, max_norm: float, norm: torch.Tensor, ws: torch.Tensor) -> None:
+    """norm[0] of a table of gradients, and their `out`s scaled so that it would be at most max_norm."""
+    _floats("norm", ws, (1,), norm)
+    _call(norm, load_library().dgnn_grad_clip, "dgnn_grad_clip", count, items, float(max_norm), _ptr(norm), *_workspace(ws, norm))
 
 
 # codes a device-side validation can leave in d_status (include/dgnn.h)

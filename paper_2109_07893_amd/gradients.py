@@ -1,0 +1,47 @@
+"""The norm over a set of gradients and their clipping (dgnn_grad_norm, dgnn_grad_clip), between the gradients that a trainer leaves
+(Section "Gradient Checkpoint") and the update of the weights.  A table of the tensors and a workspace; the arithmetic is in the HIP kernels."""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as B
+from .batch import Table
+
+
+class Gradients:
+    """Gradient tensors (float32 or bfloat16, contiguous, any shapes, on one GPU) that are looked at together, where they lie: the table
+    holds their addresses, so they are bound once and refilled by every step.  `out`: tensors of the same shapes and types that receive
+    the clipped gradients (left out: the gradients themselves)."""
+
+    G, OUT, COUNT, DT = range(4)                     # dgnn_grad_item
+
+    def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+        self.grads, self.out = list(grads), list(grads) if out is None else list(out)
+        if not self.grads or len(self.out) != len(self.grads):
+            raise ValueError("Gradients takes one tensor at least, and as many outputs")
+        dev = self.grads[0].device
+        if dev.type != "cuda":
+            raise ValueError("Gradients takes tensors on the GPU")
+        for g, o in zip(self.grads, self.out):
+            if o.shape != g.shape or o.dtype != g.dtype or g.device != dev or o.device != dev:
+                raise ValueError("shape, dtype or device mismatch in Gradients")
+        self.table = Table(len(self.grads), 4)
+        self.table.column(self.G, [B._ptr(g) or 0 for g in self.grads])
+        self.table.column(self.OUT, [B._ptr(o) or 0 for o in self.out])
+        self.table.column(self.COUNT, [g.numel() for g in self.grads])
+        self.table.column(self.DT, [B._dtype_code(g) for g in self.grads])
+        self.result = torch.zeros(1, dtype=torch.float32, device=dev)
+        self.scalar = self.result[0]
+        self.ws = torch.empty(B.grad_clip_workspace(len(self.grads)), dtype=torch.uint8, device=dev)
+
+    def norm(self) -> torch.Tensor:
+        """sqrt(sum g^2) over all of them: a scalar on the device, overwritten by the next call."""
+        B.grad_norm(len(self.grads), self.table.at(), self.result, self.ws)
+        return self.scalar
+
+    def clip(self, max_norm: float) -> torch.Tensor:
+        """out = g min(1, max_norm / (norm + 1e-6)); returns the norm from before.  A norm that is no finite number changes nothing."""
+        B.grad_clip(len(self.grads), self.table.at(), max_norm, self.result, self.ws)
+        return self.scalar

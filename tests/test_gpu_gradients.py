@@ -1,0 +1,137 @@
+"""The norm over a set of gradients and their clipping against 64 bits.
+
+Tolerances.  Squares of fp32 and bf16 numbers are exact in 64 bits and sums of up to 2^31 of them are off by 2^-52 times a small number of
+levels, so the norm is the exact one rounded to fp32 (half a step of it, 2^-24, and 2^-40 for the sums); the factor is rounded once
+(2^-24), its product with a gradient once more in the gradient's type."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2109_07893_amd as dg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def make(sizes, scale=1.0, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return [(scale * torch.randn(s, generator=g, device=DEV)).to(dt) for s, dt in sizes]
+
+
+def norm_of(grads):
+    return float(np.sqrt(sum(float((g.double() ** 2).sum()) for g in grads)))
+
+
+def check(grads, max_norm, in_place):
+    before = [g.clone() for g in grads]
+    norm = norm_of(grads)
+    out = None if in_place else [torch.full_like(g, float("nan")) for g in grads]
+    set_ = dg.Gradients(grads, out)
+    assert abs(float(set_.norm()) - norm) <= norm * (2.0 ** -24 + 2.0 ** -40)
+    assert all(torch.equal(a, b) for a, b in zip(grads, before))
+    assert abs(float(set_.clip(max_norm)) - norm) <= norm * (2.0 ** -24 + 2.0 ** -40)
+    factor = min(1.0, max_norm / (norm + 1e-6))
+    for a, b in zip(before, grads if in_place else out):
+        if factor == 1.0:
+            assert torch.equal(a, b)
+            continue
+        want = a.double() * factor
+        half = torch.finfo(a.dtype).eps / 2
+        assert bool(((b.double() - want).abs() <= want.abs() * (half + 2.0 ** -24) * (1 + 2.0 ** -10) + 1e-44).all())
+    if not in_place:
+        assert all(torch.equal(a, b) for a, b in zip(grads, before))
+
+
+SETS = {
+    "one element": [((1,), F32)],
+    "one tensor": [((77, 13), F32)],
+    "nothing in some": [((0,), F32), ((3,), BF16), ((0, 5), BF16), ((1,), F32), ((0,), F32)],
+    "around a stretch": [((8191,), F32), ((8192,), F32), ((8193,), BF16), ((16384,), BF16), ((3,), F32)],
+    "a model": [((64, 128), F32), ((128,), F32), ((32, 32), F32), ((96, 128), BF16), ((2 ** 18 + 5, 16), F32)],
+    "many": [((k % 37 + 1, k % 5 + 1), BF16 if k % 3 else F32) for k in range(300)],
+}
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("name", list(SETS))
+@pytest.mark.parametrize("max_norm", [0.01, 1e9])
+def test_clip(name, max_norm, in_place):
+    check(make(SETS[name]), max_norm, in_place)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3, 5])
+def test_addresses(shift):
+    """Gradients that begin anywhere, outputs that begin elsewhere."""
+    base, other = make([((20000,), F32)])[0], torch.zeros(20000, device=DEV)
+    check([base[shift:shift + 9000]], 1.0, True)
+    half = make([((20000,), BF16)])[0]
+    check([half[shift:shift + 17000]], 1.0, True)
+    g, out = base[shift:shift + 10001], other[shift + 1:shift + 10002]
+    dg.Gradients([g], [out]).clip(1e9)
+    assert torch.equal(g, out) and not other[:shift + 1].any() and not other[shift + 10002:].any()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-22, 1e18, 1e30])
+def test_squares_leave_32_bits(scale):
+    check(make([((5000,), F32), ((123,), BF16)], scale=scale), 0.5, True)
+
+
+def test_zero_gradients():
+    check([torch.zeros(100, device=DEV), torch.zeros(7, dtype=BF16, device=DEV)], 1.0, True)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_not_finite_changes_nothing(value):
+    grads = make([((5000,), F32), ((300,), BF16)])
+    grads[0][4321] = value
+    before = [g.clone() for g in grads]
+    out = [torch.zeros_like(g) for g in grads]
+    norm = dg.Gradients(grads, out).clip(0.1)
+    assert not torch.isfinite(norm)
+    dg.Gradients(grads).clip(0.1)
+    for a, b, c in zip(before, grads, out):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+
+
+def test_refusals():
+    g = torch.ones(64, device=DEV)
+    for grads, out in (([g, g], None), ([g[:40], g[30:]], None), ([g, torch.ones(64, device=DEV)], [torch.empty(64, device=DEV), g])):
+        with pytest.raises(dg.DgnnError):
+            dg.Gradients(grads, out).clip(1.0)
+    assert float(dg.Gradients([g, g]).norm()) == pytest.approx(128 ** 0.5, rel=2 ** -22)       # the norm alone writes nothing
+    with pytest.raises(dg.DgnnError):
+        dg.Gradients([g]).clip(0.0)
+    with pytest.raises(ValueError):
+        dg.Gradients([g], [torch.empty(63, device=DEV)])
+    assert bool((g == 1).all())
+
+
+def test_large_tensor():
+    """More than 2^31 elements."""
+    n = (1 << 31) + 12345
+    g = torch.zeros(n, dtype=BF16, device=DEV)
+    g[:3], g[-3:] = 2.0, 4.0
+    set_ = dg.Gradients([g])
+    assert float(set_.norm()) == pytest.approx(60 ** 0.5, rel=2 ** -22)
+    set_.clip(60 ** 0.5 / 2)
+    assert g[:3].tolist() == [1.0] * 3 and g[-4:].tolist() == [0.0, 2.0, 2.0, 2.0]
+
+
+def test_repeats_and_graph():
+    grads = make(SETS["many"] + SETS["a model"], seed=3)
+    out = [torch.empty_like(g) for g in grads]
+    set_ = dg.Gradients(grads, out)
+    norm = set_.clip(0.7).clone()
+    eager = [o.clone() for o in out]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        set_.clip(0.7)
+    for _ in range(3):
+        for o in out:
+            o.zero_()
+        set_.result.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(set_.scalar, norm) and all(torch.equal(a, b) for a, b in zip(out, eager))
+        dg.Gradients(grads[:5]).norm()
