@@ -725,7 +725,7 @@ int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bia
  *   a [f][N]; d [f], dt_bias [f] or NULL (zero)
  *   h_before [n][f][N] fp32      the state ahead of the series, or NULL (zero)
  *   h_after [n][f][N] fp32       receives the last state, or NULL; may be h_before
- *   checkpoints                  NULL, or fp32 of dgnn_selective_scan_checkpoints() bytes: the state ahead of every 16th timestep,
+ *   checkpoints                  NULL, or fp32 of dgnn_selective_scan_checkpoints() bytes: the state ahead of every 8th timestep,
  *                                which is what the adjoint needs of the forward pass
  *   ws                           dgnn_selective_scan_workspace() bytes, 16-byte aligned
  * States, step sizes and sums are fp32, y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose

@@ -948,7 +948,7 @@ def _scan_args(name, x, delta, bc, z, a, d, dt_bias, checkpoints, lengths):
     _lengths(lengths, x)
     if checkpoints is not None:
         _need(checkpoints, torch.float32, "checkpoints")
-        if checkpoints.device != x.device or checkpoints.numel() < (T + 15) // 16 * n * f * states:
+        if checkpoints.device != x.device or checkpoints.numel() < selective_scan_checkpoints(T, n, f, states):
             raise DgnnError(-3, f"{name} (checkpoints)")
     return T, n, f, states
 

@@ -12,6 +12,11 @@
 // modifiers.  Sums over a channel's states stay inside the four lanes; four timesteps' sums are exchanged at once and end in the lane
 // whose timestep they are.  Sums over channels (dB, dC) run across the sixteen groups of four, again many at a time, so that every step
 // of the exchange halves the number of registers; the wavefronts of a sequence then meet in LDS.
+//
+// The time axis goes by tiles of sixteen steps.  B and C of a tile are the same for all channels: a wavefront fetches them as whole
+// 16-byte pieces and reads them back from LDS, four addresses a read, where a load per timestep would keep the 64 lanes of the
+// cache's port busy for 64 bytes.  Wavefronts stay, keep their channels (and so a, d and the bias) and take one sequence after the other;
+// the loads of the next tile, be it of the next sequence, are under way while a tile is computed.
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -24,11 +29,11 @@ namespace {
 using namespace dgnn;
 
 constexpr int kChannels = 16;             // channels of a wavefront
-constexpr int kTile = 16;                 // timesteps between two kept states (and of a piece of the time axis at least)
+constexpr int kTile = 16;                 // timesteps of a tile
+constexpr int kHeld = 8;                  // ... between two kept states: the adjoint holds the states of so many in registers
 constexpr int kWaves = 4;                 // wavefronts of a workgroup of the kernels without sums over channels
 constexpr int kBackWaves = 8;             // ... of the adjoint, at most
-constexpr int kMaxGrid = 1 << 22;         // workgroups of a launch: HIP counts its threads in 32 bits
-constexpr int kMaxSlots = 1024;           // workgroups of the adjoint that leave sums over time and sequences
+constexpr int kBackResident = 2048;       // ... of all its workgroups: two on a SIMD
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;
 constexpr float kLn2 = 0.693147180559945309417f;
@@ -53,7 +58,7 @@ struct ScanBack {
     float *dh_before;
     float *dbc_part;                      // [blocks of channel groups][T][n][2 N], where a sequence has more than one workgroup
     double *sums;                         // [slots][f (N + 2)]: da, dd, ddt_bias
-    int blocks_of_groups, sequences;      // workgroups of a sequence; sequences of a workgroup
+    int blocks_of_groups;                 // workgroups of a sequence
 };
 
 // ---- arithmetic ---------------------------------------------------------------------------------------------------
@@ -68,20 +73,18 @@ __device__ __forceinline__ float exp_of(float v) {
     return p < -160.0f ? 0.0f : fmaf(e, low * kLn2, e);
 }
 
-// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), and sig(v).  log(1 + e) = 2 artanh(e / (2 + e)) by its power series: the argument
-// is at most 1/3, eight terms leave 1.4e-9 of the result, and a small e loses no digits, which 1 + e would.
+// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), and sig(v).  log(1 + e) = 2 artanh(r) with r = e / (2 + e) <= 1/3, an odd series:
+// r P(r^2) with the polynomial of degree 4 that meets it at the Chebyshev nodes of [0, 1/9], 4e-9 of the result off.  A small e loses no
+// digits, which 1 + e would.
 __device__ __forceinline__ float softplus_of(float v, float &sig) {
     const float e = exp_of(-fabsf(v));
     const float r = e * rcp_of(2.0f + e), q = r * r;
-    float p = fmaf(q, 1.0f / 15, 1.0f / 13);
-    p = fmaf(p, q, 1.0f / 11);
-    p = fmaf(p, q, 1.0f / 9);
-    p = fmaf(p, q, 1.0f / 7);
-    p = fmaf(p, q, 1.0f / 5);
-    p = fmaf(p, q, 1.0f / 3);
-    p = fmaf(p, q, 1.0f);
+    float p = fmaf(q, 0.28157778f, 0.27965158f);
+    p = fmaf(p, q, 0.40024595f);
+    p = fmaf(p, q, 0.66666322f);
+    p = fmaf(p, q, 2.00000001f);
     sig = (v >= 0.0f ? 1.0f : e) * rcp_of(1.0f + e);
-    return fmaxf(v, 0.0f) + 2.0f * r * p;
+    return fmaf(r, p, fmaxf(v, 0.0f));
 }
 __device__ __forceinline__ float sigmoid_of(float v) { return rcp_of(1.0f + exp2_of(-v * kLog2e)); }
 
@@ -180,27 +183,21 @@ template <int S> __device__ __forceinline__ void store_state(float *p, const flo
     }
 }
 
-// Item i = sequence * groups + group of channels.
-__device__ __forceinline__ void split_item(int64_t i, int groups, int64_t &v, int &g) {
-    if ((i >> 32) == 0) { v = (uint32_t)i / (uint32_t)groups; g = (uint32_t)i % (uint32_t)groups; }
-    else { v = i / groups; g = (int)(i % groups); }
-}
-
 __device__ __forceinline__ int length_of(const int32_t *lengths, int64_t v, int T) {
     return lengths ? min(max(uniform(lengths[v]), 0), T) : T;
 }
 
-// What a wavefront's lane has of one sequence: its channel, its states, where its rows lie.
-template <bool BF16, int S> struct Lane {
-    typedef typename Elem<BF16>::Type E;
+// What a wavefront's lane is: its channel, its quarter of the states, and where its values lie in the frames.
+template <int S> struct Lane {
     static constexpr int N = 4 * S;
-    int q, ch;
-    int64_t v, n, f;
-    __device__ __forceinline__ Lane(const Scan &s, int64_t v_, int g, int lane) : q(lane & 3), ch(g * kChannels + (lane >> 2)), v(v_), n(s.n), f(s.f) {}
-    __device__ __forceinline__ int64_t at(int t) const { return ((int64_t)t * n + v) * f + ch; }                     // of a frame [T][n][f]
-    __device__ __forceinline__ const E *b_row(const void *bc, int t) const { return static_cast<const E *>(bc) + ((int64_t)t * n + v) * 2 * N + q * S; }
-    __device__ __forceinline__ int64_t state(int64_t piece) const { return (((piece * n + v) * f) + ch) * N + q * S; }
-    __device__ __forceinline__ int64_t channel(int64_t piece) const { return (piece * n + v) * f + ch; }
+    int q, ch, lane;
+    int64_t n, f, own;                    // own: the lane's place relative to the first of four timesteps in [T][n][f]
+    __device__ __forceinline__ Lane(const Scan &s, int g, int lane_) : q(lane_ & 3), ch(g * kChannels + (lane_ >> 2)), lane(lane_), n(s.n), f(s.f) {
+        own = (int64_t)q * n * f + ch;
+    }
+    __device__ __forceinline__ int64_t at(int64_t v, int t) const { return ((int64_t)t * n + v) * f + own; }          // of timestep t + q
+    __device__ __forceinline__ int64_t state(int64_t piece, int64_t v) const { return (((piece * n + v) * f) + ch) * N + q * S; }
+    __device__ __forceinline__ int64_t channel(int64_t piece, int64_t v) const { return (piece * n + v) * f + ch; }
 };
 
 // a log2(e) of a lane's states: e = 2^(dt a2).
@@ -209,138 +206,237 @@ template <int S> __device__ __forceinline__ void load_decay(float (&a2)[S], cons
     for (int s = 0; s < S; ++s) a2[s] = a[(int64_t)ch * 4 * S + q * S + s] * kLog2e;
 }
 
-// The state ahead of piece p: what its predecessors leave, each taken from zero by scan_piece_kernel (the first from h_before).
-template <bool BF16, int S>
-__device__ __forceinline__ void join_pieces(float (&h)[S], const float (&a2)[S], const Scan &s, const Lane<BF16, S> &l, int p) {
-    if (p == 0) { load_state(h, s.piece_state + l.state(s.pieces - 1)); return; }
-    load_state(h, s.piece_state + l.state(0));
-    for (int k = 1; k < p; ++k) {
-        float part[S];
-        load_state(part, s.piece_state + l.state(k));
-        const float time = s.piece_time[l.channel(k)];
-#pragma unroll
-        for (int i = 0; i < S; ++i) h[i] = fmaf(exp2_of(time * a2[i]), h[i], part[i]);
+// Sequence v in piece p of the time axis: timesteps [t0, t1), of which the sequence has those ahead of t_end.
+struct Place {
+    int64_t v;
+    int p, t0, t1, t_end;
+    __device__ __forceinline__ bool settle(const Scan &s, int pieces) {          // after v was moved on
+        while (v >= s.n) { v -= s.n; ++p; }
+        if (p >= pieces) return false;
+        t0 = p * s.chunk;
+        t1 = min(s.T, t0 + s.chunk);
+        t_end = min(t1, length_of(s.lengths, v, s.T));
+        return true;
     }
-}
-
-// ---- forward ------------------------------------------------------------------------------------------------------
-// Four timesteps of a wavefront as they lie in memory.
-template <bool BF16, int S> struct Four {
-    float x, delta, z, b[4][S], c[4][S];
 };
 
-// Y = whether outputs are formed (else only the state is carried along); `steps` of the four exist.
-template <bool BF16, int S, bool Y>
-__device__ __forceinline__ void load_four(Four<BF16, S> &r, const Scan &s, const Lane<BF16, S> &l, int t, int steps) {
+// B and C of a tile of K timesteps on their way to LDS: 16-byte pieces of its rows, in order over the lanes.
+template <bool BF16, int S, int K> struct Rows {
     typedef typename Elem<BF16>::Type E;
-    const int64_t at = l.at(t + min(l.q, steps - 1));
-    r.x = Elem<BF16>::get(static_cast<const E *>(s.x) + at);
-    r.delta = Elem<BF16>::get(static_cast<const E *>(s.delta) + at);
-    if (Y) r.z = s.z ? Elem<BF16>::get(static_cast<const E *>(s.z) + at) : 0.0f;
+    static constexpr int kValues = 16 / sizeof(E), kRow = 8 * S / kValues;        // values of a piece, pieces of a row
+    static constexpr int kPieces = K * kRow, kLoads = (kPieces + kWave - 1) / kWave;
+    uintx4 r[kLoads];
+    __device__ __forceinline__ void load(const void *bc, int64_t n, int64_t v, int t, int steps, int lane) {
+        const uintx4 *const p = static_cast<const uintx4 *>(bc) + ((int64_t)t * n + v) * kRow;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const E *row = l.b_row(s.bc, t + min(j, steps - 1));
-        Elem<BF16>::template row<S>(r.b[j], row);
-        if (Y) Elem<BF16>::template row<S>(r.c[j], row + 4 * S);
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = i * kWave + lane, row = at / kRow;
+            r[i] = uintx4{0, 0, 0, 0};                                            // rows behind the sequence: nothing
+            if (row < steps) r[i] = p[(int64_t)row * n * kRow + at % kRow];
+        }
     }
+    __device__ __forceinline__ void stage(float *to, int lane) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = i * kWave + lane;
+            if (kPieces % kWave == 0 || at < kPieces) {
+                float v[kValues];
+                Pack<BF16>::unpack(v, r[i]);
+#pragma unroll
+                for (int k = 0; k < kValues; k += 4) *reinterpret_cast<uintx4 *>(to + at * kValues + k) = Pack<false>::pack({v[k], v[k + 1], v[k + 2], v[k + 3]});
+            }
+        }
+    }
+};
+
+// ---- forward ------------------------------------------------------------------------------------------------------
+template <bool BF16, int S> struct Tile {
+    Rows<BF16, S, kTile> rows;
+    float x[kTile / 4], delta[kTile / 4], z[kTile / 4], h[S];
+};
+
+// The tile of `steps` timesteps from t on; the state ahead of it where it is the first one of a series that is not cut into pieces.
+template <bool BF16, int S, bool Y, bool GATE>
+__device__ __forceinline__ void load_tile(Tile<BF16, S> &r, const Scan &s, const Lane<S> &l, int64_t v, int t, int steps, bool first) {
+    typedef typename Elem<BF16>::Type E;
+    r.rows.load(s.bc, s.n, v, t, steps, l.lane);
+    const int64_t at = l.at(v, t), four = 4 * s.n * s.f;
+#pragma unroll
+    for (int i = 0; i < kTile / 4; ++i)
+        if (4 * i + l.q < steps) {
+            r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at + i * four);
+            r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at + i * four);
+            if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at + i * four);
+        }
+    if (first && s.h_before && (Y ? s.pieces == 1 : t == 0)) load_state(r.h, s.h_before + l.state(0, v));
+    else if (first)
+#pragma unroll
+        for (int k = 0; k < S; ++k) r.h[k] = 0.0f;
 }
 
-template <bool BF16, int S, bool Y, int J>
-__device__ __forceinline__ void one_step(float (&h)[S], float &out, const float (&a2)[S], const Four<BF16, S> &r, float dt, float dtx) {
+template <int S, bool Y, int J>
+__device__ __forceinline__ float one_step(float (&h)[S], const float (&a2)[S], const float *row, float dt, float dtx) {
+    float b[S], c[S], acc = 0.0f;
+    load_state(b, row);
+    if (Y) load_state(c, row + 4 * S);
     const float dt_j = of_lane<J>(dt), dtx_j = of_lane<J>(dtx);
-    float acc = 0.0f;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-        h[i] = fmaf(exp2_of(dt_j * a2[i]), h[i], dtx_j * r.b[J][i]);
-        if (Y) acc = fmaf(r.c[J][i], h[i], acc);
+        h[i] = fmaf(exp2_of(dt_j * a2[i]), h[i], dtx_j * b[i]);
+        if (Y) acc = fmaf(c[i], h[i], acc);
     }
-    out = acc;
+    return acc;
 }
 
-template <bool BF16, int S, bool Y>
-__device__ __forceinline__ void four_steps(float (&h)[S], float &time, const float (&a2)[S], const Scan &s, const Lane<BF16, S> &l, const Four<BF16, S> &r, int t,
-                                           int steps, float bias, float d) {
+// Y: outputs are formed (GATE: under z).  Else only what a piece of the time axis leaves behind when it starts from zero (the first: from h_before), and
+// the sum of its step sizes, which gives the decay across it, exp(a sum dt).
+template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void scan_tiles(const Scan &s, float *s_rows) {
     typedef typename Elem<BF16>::Type E;
-    float sig;
-    const float dt = softplus_of(r.delta + bias, sig), dtx = dt * r.x;
-    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    one_step<BF16, S, Y, 0>(h, out[0], a2, r, dt, dtx);
-    if (steps > 1) one_step<BF16, S, Y, 1>(h, out[1], a2, r, dt, dtx);
-    if (steps > 2) one_step<BF16, S, Y, 2>(h, out[2], a2, r, dt, dtx);
-    if (steps > 3) one_step<BF16, S, Y, 3>(h, out[3], a2, r, dt, dtx);
-    if (!Y) time += l.q < steps ? dt : 0.0f;
-    else {
-        float y = fmaf(d, r.x, quad_sums(out, l.q));
-        if (s.z) y *= r.z * sigmoid_of(r.z);
-        if (l.q < steps) Elem<BF16>::put(static_cast<E *>(s.y) + l.at(t + l.q), y);
-    }
-}
-
-// One sequence's sixteen channels over [t0, t_end), the states of four timesteps ahead of their use.
-template <bool BF16, int S, bool Y>
-__device__ __forceinline__ void walk(float (&h)[S], float &time, const float (&a2)[S], const Scan &s, const Lane<BF16, S> &l, int t0, int t_end, float bias, float d) {
-    if (t0 >= t_end) return;
-    Four<BF16, S> now, next;
-    load_four<BF16, S, Y>(now, s, l, t0, min(4, t_end - t0));
-    for (int t = t0; t < t_end; t += 4) {
-        if (Y && s.checkpoints && (t & (kTile - 1)) == 0) store_state(s.checkpoints + l.state(t / kTile), h);
-        const int left = t_end - t;
-        if (left > 4) load_four<BF16, S, Y>(next, s, l, t + 4, min(4, left - 4));
-        if (left >= 4) four_steps<BF16, S, Y>(h, time, a2, s, l, now, t, 4, bias, d);
-        else four_steps<BF16, S, Y>(h, time, a2, s, l, now, t, left, bias, d);
-        now = next;
-    }
-}
-
-template <bool BF16, int S>
-__global__ __launch_bounds__(kWaves *kWave) void scan_kernel(Scan s) {
-    typedef typename Elem<BF16>::Type E;
-    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), p = blockIdx.y;
-    const int t0 = p * s.chunk, t1 = min(s.T, t0 + s.chunk);
-    for (int64_t i = (int64_t)blockIdx.x * kWaves + wave; i < s.n * s.groups; i += (int64_t)gridDim.x * kWaves) {
-        int64_t v;
-        int g;
-        split_item(i, s.groups, v, g);
-        const Lane<BF16, S> l(s, v, g, lane);
-        const int t_end = min(t1, length_of(s.lengths, v, s.T));
-        float a2[S], h[S], time = 0.0f;
-        load_decay(a2, s.a, l.ch, l.q);
-        const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f, d = s.d ? s.d[l.ch] : 0.0f;
-        if (s.pieces > 1) join_pieces<BF16, S>(h, a2, s, l, p);
-        else if (s.h_before) load_state(h, s.h_before + l.state(0));
-        else
+    constexpr int N = 4 * S;
+    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), pieces = Y ? s.pieces : s.pieces - 1;
+    const int w = blockIdx.x * kWaves + wave, stride = (int)(gridDim.x * kWaves) / s.groups;
+    if (w / s.groups >= stride) return;
+    float *const rows = s_rows + wave * 2 * kTile * 2 * N;
+    const Lane<S> l(s, w % s.groups, lane);
+    float a2[S], h[S], time = 0.0f;
+    load_decay(a2, s.a, l.ch, l.q);
+    const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f, d = s.d ? s.d[l.ch] : 0.0f;
+    Place here{w / s.groups, 0, 0, 0, 0};
+    if (!here.settle(s, pieces)) return;
+    int t = here.t0, buffer = 0;
+    // Loads of a tile -> what is computed with.  Loads and stores leave a wavefront in one order and are counted in it, so waiting for a
+    // load is waiting for every store ahead of it too: the next tile's loads go out first, are taken up after all of this tile's arithmetic,
+    // and this tile's stores follow.
+    Tile<BF16, S> r;
+    float x[kTile / 4], z[kTile / 4], dt[kTile / 4], start[S];
+    auto take = [&](int steps, int to) {
+        r.rows.stage(rows + to * kTile * 2 * N, lane);
 #pragma unroll
-            for (int k = 0; k < S; ++k) h[k] = 0.0f;
-        walk<BF16, S, true>(h, time, a2, s, l, t0, t_end, bias, d);
-        for (int t = max(t0, t_end) + l.q; t < t1; t += 4) Elem<BF16>::put(static_cast<E *>(s.y) + l.at(t), 0.0f);
-        if (s.h_after && p == s.pieces - 1) store_state(s.h_after + l.state(0), h);
+        for (int i = 0; i < kTile / 4; ++i)
+            if (4 * i < steps) {
+                float sig;
+                x[i] = r.x[i];
+                if (GATE) z[i] = r.z[i];
+                dt[i] = softplus_of(r.delta[i] + bias, sig);
+            }
+#pragma unroll
+        for (int k = 0; k < S; ++k) start[k] = r.h[k];
+    };
+    load_tile<BF16, S, Y, GATE>(r, s, l, here.v, t, min(kTile, here.t_end - t), true);
+    take(min(kTile, here.t_end - t), 0);
+    for (;;) {
+        const int steps = min(kTile, here.t_end - t);
+        Place next = here;
+        int t_next = t + kTile;
+        bool more = true;
+        if (t_next >= here.t_end) {
+            next.v += stride;
+            more = next.settle(s, pieces);
+            t_next = next.t0;
+        }
+        if (t == here.t0) {
+            if (Y && s.pieces > 1) {      // what its predecessors leave (join_kernel)
+                load_state(h, s.piece_state + l.state(here.p == 0 ? s.pieces - 1 : here.p - 1, here.v));
+            } else
+#pragma unroll
+                for (int k = 0; k < S; ++k) h[k] = start[k];
+            // A copy of the first piece's state ahead lies where the last one's would: the last piece's wavefront may write h_after over
+            // h_before before the first one's reads it.
+            if (!Y && here.p == 0) store_state(s.piece_state + l.state(s.pieces - 1, here.v), h);
+            time = 0.0f;
+        }
+        if (Y && s.checkpoints && steps > 0) store_state(s.checkpoints + l.state(t / kHeld, here.v), h);
+        if (more) load_tile<BF16, S, Y, GATE>(r, s, l, next.v, t_next, min(kTile, next.t_end - t_next), t_next == next.t0);
+        wave_lds_sync();
+        float y[kTile / 4], half[S];
+        auto group = [&](int i, int left) {                 // four timesteps, of which `left` are there
+            const float *const row = rows + buffer * kTile * 2 * N + 4 * i * 2 * N + l.q * S;
+            const float dtx = dt[i] * x[i];
+            if (kHeld < kTile && i == 2)
+#pragma unroll
+                for (int k = 0; k < S; ++k) half[k] = h[k];
+            float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            out[0] = one_step<S, Y, 0>(h, a2, row, dt[i], dtx);
+            if (left > 1) out[1] = one_step<S, Y, 1>(h, a2, row + 2 * N, dt[i], dtx);
+            if (left > 2) out[2] = one_step<S, Y, 2>(h, a2, row + 4 * N, dt[i], dtx);
+            if (left > 3) out[3] = one_step<S, Y, 3>(h, a2, row + 6 * N, dt[i], dtx);
+            if (Y) {
+                y[i] = fmaf(d, x[i], quad_sums(out, l.q));
+                if (GATE) y[i] *= z[i] * sigmoid_of(z[i]);
+            } else time += l.q < left ? dt[i] : 0.0f;
+        };
+        if (steps == kTile) {
+#pragma unroll
+            for (int i = 0; i < kTile / 4; ++i) group(i, 4);
+        } else
+#pragma unroll
+            for (int i = 0; i < kTile / 4; ++i)
+                if (4 * i < steps) group(i, steps - 4 * i);
+        if (more) take(min(kTile, next.t_end - t_next), buffer ^ 1);
+        if (Y) {
+            const int64_t at = l.at(here.v, t), four = 4 * s.n * s.f;
+            if (steps == kTile) {
+#pragma unroll
+                for (int i = 0; i < kTile / 4; ++i) Elem<BF16>::put(static_cast<E *>(s.y) + at + i * four, y[i]);
+            } else
+#pragma unroll
+                for (int i = 0; i < kTile / 4; ++i)
+                    if (4 * i + l.q < steps) Elem<BF16>::put(static_cast<E *>(s.y) + at + i * four, y[i]);
+            if (kHeld < kTile && s.checkpoints && steps > kHeld) store_state(s.checkpoints + l.state(t / kHeld + 1, here.v), half);
+        }
+        if (t + kTile >= here.t_end) {    // the sequence ends here, or this piece of it
+            if (Y) {
+                for (int o = max(here.t0, here.t_end); o < here.t1; o += 4)
+                    if (o + l.q < here.t1) Elem<BF16>::put(static_cast<E *>(s.y) + l.at(here.v, o), 0.0f);
+                if (s.h_after && here.p == s.pieces - 1) store_state(s.h_after + l.state(0, here.v), h);
+            } else {
+                time = quad_sum(time);
+                store_state(s.piece_state + l.state(here.p, here.v), h);
+                if (l.q == 0) s.piece_time[l.channel(here.p, here.v)] = time;
+            }
+        }
+        if (!more) return;
+        here = next;
+        t = t_next;
+        buffer ^= 1;
     }
 }
 
-// Where there are few sequences the time axis is cut into pieces: what each leaves when it starts from zero (the first: from h_before),
-// and the sum of its step sizes, which gives the decay across it, exp(a sum dt).  The last piece's place takes a copy of h_before: the
-// last piece's wavefront may write h_after over it before the first one's has read it.
-template <bool BF16, int S>
-__global__ __launch_bounds__(kWaves *kWave) void scan_piece_kernel(Scan s) {
-    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), p = blockIdx.y;
-    const int t0 = p * s.chunk, t1 = min(s.T, t0 + s.chunk);
-    for (int64_t i = (int64_t)blockIdx.x * kWaves + wave; i < s.n * s.groups; i += (int64_t)gridDim.x * kWaves) {
-        int64_t v;
-        int g;
-        split_item(i, s.groups, v, g);
-        const Lane<BF16, S> l(s, v, g, lane);
-        const int t_end = min(t1, length_of(s.lengths, v, s.T));
-        float a2[S], h[S], time = 0.0f;
-        load_decay(a2, s.a, l.ch, l.q);
-        if (p == 0 && s.h_before) load_state(h, s.h_before + l.state(0));
-        else
+template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWave) void scan_kernel(Scan s) {
+    __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
+    scan_tiles<BF16, S, true, GATE>(s, s_rows);
+}
+// Where there are few sequences the time axis is cut into pieces, and this goes ahead over all but the last one.
+template <bool BF16, int S> __global__ __launch_bounds__(kWaves *kWave) void scan_piece_kernel(Scan s) {
+    __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
+    scan_tiles<BF16, S, false, false>(s, s_rows);
+}
+
+// The states between the pieces, in place.  Forward (STEP 1): piece p left part[p] behind when it started from zero, part[0] from h_before;
+// the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
+// reaches piece p from behind takes the place p + 1.  A lane has one state and fetches kJoin pieces' parts together.
+constexpr int kJoin = 16;
+template <int STEP> __global__ __launch_bounds__(256) void join_kernel(Scan s, const float *behind, int states) {
+    const int64_t width = s.n * s.f * states, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= width) return;
+    const int64_t c = i / states;
+    const float a2 = s.a[c % s.f * states + i % states] * kLog2e;
+    const int first = STEP > 0 ? 1 : s.pieces - 1, count = s.pieces - (STEP > 0 ? 2 : 1);
+    float h = STEP > 0 ? s.piece_state[i] : behind ? behind[i] : 0.0f;
+    for (int k = 0; k < count; k += kJoin) {
+        float part[kJoin], time[kJoin];
 #pragma unroll
-            for (int k = 0; k < S; ++k) h[k] = 0.0f;
-        if (p == 0) store_state(s.piece_state + l.state(s.pieces - 1), h);
-        walk<BF16, S, false>(h, time, a2, s, l, t0, t_end, s.dt_bias ? s.dt_bias[l.ch] : 0.0f, 0.0f);
-        time = quad_sum(time);
-        store_state(s.piece_state + l.state(p), h);
-        if (l.q == 0) s.piece_time[l.channel(p)] = time;
+        for (int j = 0; j < kJoin; ++j) {
+            const int p = first + STEP * min(k + j, count - 1);
+            part[j] = s.piece_state[p * width + i];
+            time[j] = s.piece_time[p * s.n * s.f + c];
+        }
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j)
+            if (k + j < count) {
+                h = fmaf(exp2_of(time[j] * a2), h, part[j]);
+                s.piece_state[(first + STEP * (k + j)) * width + i] = h;
+            }
     }
 }
 
@@ -349,23 +445,22 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_piece_kernel(Scan s) {
 template <bool BF16, int S>
 __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
+    constexpr int N = 4 * S;
     const Scan &s = b.s;
-    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), p = blockIdx.y + 1;
-    const int t0 = p * s.chunk, t1 = min(s.T, t0 + s.chunk);
-    for (int64_t i = (int64_t)blockIdx.x * kWaves + wave; i < s.n * s.groups; i += (int64_t)gridDim.x * kWaves) {
-        int64_t v;
-        int g;
-        split_item(i, s.groups, v, g);
-        const Lane<BF16, S> l(s, v, g, lane);
-        const int t_end = min(t1, length_of(s.lengths, v, s.T));
-        const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f;
-        float a2[S], k[S], time = 0.0f;
-        load_decay(a2, s.a, l.ch, l.q);
+    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
+    const int w = blockIdx.x * kWaves + wave, stride = (int)(gridDim.x * kWaves) / s.groups;
+    if (w / s.groups >= stride) return;
+    const Lane<S> l(s, w % s.groups, lane);
+    const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f;
+    float a2[S];
+    load_decay(a2, s.a, l.ch, l.q);
+    for (Place here{w / s.groups, 1, 0, 0, 0}; here.settle(s, s.pieces); here.v += stride) {
+        float k[S], time = 0.0f;
 #pragma unroll
-        for (int i2 = 0; i2 < S; ++i2) k[i2] = 0.0f;
+        for (int i = 0; i < S; ++i) k[i] = 0.0f;
         auto four = [&](int t, int steps) {
             const bool there = l.q < steps;
-            const int64_t at = l.at(t + min(l.q, steps - 1));
+            const int64_t at = l.at(here.v, t) - (there ? 0 : (int64_t)(l.q - (steps - 1)) * s.n * s.f);
             float sig, gy = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at);
             if (s.z) {
                 const float z = Elem<BF16>::get(static_cast<const E *>(s.z) + at);
@@ -375,7 +470,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
             time += there ? dt : 0.0f;
             auto step = [&](float dt_j, float g_j, int j) {
                 float c[S];
-                Elem<BF16>::template row<S>(c, l.b_row(s.bc, t + j) + 4 * S);
+                Elem<BF16>::template row<S>(c, static_cast<const E *>(s.bc) + (((int64_t)(t + j) * s.n + here.v) * 2 + 1) * N + l.q * S);
 #pragma unroll
                 for (int m = 0; m < S; ++m) k[m] = exp2_of(dt_j * a2[m]) * fmaf(c[m], g_j, k[m]);
             };
@@ -384,241 +479,295 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
             if (steps > 1) step(of_lane<1>(dt), of_lane<1>(gy), 1);
             step(of_lane<0>(dt), of_lane<0>(gy), 0);
         };
-        int t = t0 + ((t_end - t0 - 1) & ~3);
-        if (t_end > t0) {
-            if (t_end - t < 4) { four(t, t_end - t); t -= 4; }
-            for (; t >= t0; t -= 4) four(t, 4);
+        if (here.t_end > here.t0) {
+            int t = here.t0 + ((here.t_end - here.t0 - 1) & ~3);
+            if (here.t_end - t < 4) { four(t, here.t_end - t); t -= 4; }
+            for (; t >= here.t0; t -= 4) four(t, 4);
         }
         time = quad_sum(time);
-        store_state(s.piece_state + l.state(p), k);
-        if (l.q == 0) s.piece_time[l.channel(p)] = time;
+        store_state(s.piece_state + l.state(here.p, here.v), k);
+        if (l.q == 0) s.piece_time[l.channel(here.p, here.v)] = time;
     }
 }
 
-// Timesteps that a wavefront holds the states of: as many as fit its registers.
-template <int S> constexpr int kHeld = S <= 4 ? 16 : 8;
+// Timesteps of a tile of the adjoint: what a wavefront fetches ahead.
+template <int S> constexpr int kBackTile = S <= 4 ? 16 : 8;
+// Decays that a lane keeps in LDS on the way ahead for the way back.
+template <int S> constexpr int kDecays = S <= 4 ? kHeld * S : 0;
 
-template <bool BF16, int S>
+template <bool BF16, int S> struct BackTile {
+    static constexpr int K = kBackTile<S>;
+    Rows<BF16, S, K> rows;
+    float x[K / 4], delta[K / 4], gy[K / 4], z[K / 4], h[K / kHeld][S], k[S];
+};
+
+// `k`: what reaches the last tile of a piece from behind.
+template <bool BF16, int S, bool GATE>
+__device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanBack &b, const Lane<S> &l, const Place &p, int t, int steps, bool last) {
+    typedef typename Elem<BF16>::Type E;
+    constexpr int K = kBackTile<S>;
+    const Scan &s = b.s;
+    r.rows.load(s.bc, s.n, p.v, t, steps, l.lane);
+    const int64_t at = l.at(p.v, t), four = 4 * s.n * s.f;
+#pragma unroll
+    for (int i = 0; i < K / 4; ++i)
+        if (4 * i + l.q < steps) {
+            r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at + i * four);
+            r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at + i * four);
+            r.gy[i] = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at + i * four);
+            if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at + i * four);
+        }
+#pragma unroll
+    for (int i = 0; i < K / kHeld; ++i)
+        if (i * kHeld < steps) load_state(r.h[i], s.checkpoints + l.state(t / kHeld + i, p.v));
+    if (last && p.p < s.pieces - 1) load_state(r.k, s.piece_state + l.state(p.p + 1, p.v));
+    else if (last && b.dh_after) load_state(r.k, b.dh_after + l.state(0, p.v));
+    else if (last)
+#pragma unroll
+        for (int i = 0; i < S; ++i) r.k[i] = 0.0f;
+}
+
+// A workgroup has all channels of a sequence, or a part of them (of kBackWaves wavefronts).
+template <bool BF16, int S, bool GATE>
 __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
-    constexpr int N = 4 * S, K = kHeld<S>, R = K / 4, V = K * 2 * N;      // V: values of dB and dC of a tile
-    extern __shared__ float s_bc[];                                       // [2][wavefronts][V]
+    constexpr int N = 4 * S, K = kBackTile<S>, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
+    constexpr int J = S <= 4 ? 4 : 2;                                     // timesteps whose sums over channels are exchanged together
+    // [3][wavefronts][V], the three by turns: B and C of a tile, where dB and dC take their place timestep by timestep (the next tile's B
+    // and C are laid down when a slower wavefront may still be adding up this one's dB and dC); [wavefronts][kHeld][lanes][S] decays where
+    // they fit (17 KB a wavefront with 16 states), which take a product and an exponential each to form again; 64-bit sums.
+    extern __shared__ float s_mem[];
     const Scan &s = b.s;
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int part = blockIdx.x % b.blocks_of_groups, slot = blockIdx.x / b.blocks_of_groups, slots = gridDim.x / b.blocks_of_groups;
-    const int own = b.sequences > 1 ? s.groups : waves;                   // wavefronts of one sequence in this workgroup
-    const int g = b.blocks_of_groups > 1 ? part * kBackWaves + wave : wave % own, which = wave / own;
-    const bool in_width = g < s.groups;
-    const int ch = g * kChannels + (lane >> 2), q = lane & 3;
-    float a2[S], a[S], acc_a[S];
-    double sum_a[S], sum_d = 0.0, sum_bias = 0.0;
+    const int g = part * kBackWaves + wave, active = min(waves, s.groups - part * kBackWaves);
+    if (wave >= active) return;                                           // the last part may be narrower; a barrier waits for those that are left
+    const Lane<S> l(s, g, lane);
+    const int q = l.q, turn = waves * V;
+    float a2[S], acc[S + 2];                                              // sums over a few tiles: da of the lane's states, dd, ddt_bias
+    load_decay(a2, s.a, l.ch, q);
+    float *const decays = s_mem + 3 * turn + wave * kDecays<S> * kWave + lane * S;
+    double *const sums = reinterpret_cast<double *>(s_mem + 3 * turn + waves * kDecays<S> * kWave) + wave * (S + 2) * kWave + lane;
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-        a[i] = in_width ? s.a[(int64_t)ch * N + q * S + i] : 0.0f;
-        a2[i] = a[i] * kLog2e;
-        sum_a[i] = 0.0;
-    }
-    const float bias = s.dt_bias && in_width ? s.dt_bias[ch] : 0.0f, d = s.d && in_width ? s.d[ch] : 0.0f;
-    const int64_t items = (s.n + b.sequences - 1) / b.sequences * s.pieces;
-    int buffer = 0;
-    for (int64_t item = slot; item < items; item += slots) {
-        const int p = (int)(item % s.pieces);
-        const int64_t first = item / s.pieces * b.sequences, v = first + which;
-        const int t0 = p * s.chunk, t1 = min(s.T, t0 + s.chunk);
-        const bool mine = in_width && v < s.n;
-        const Lane<BF16, S> l(s, mine ? v : 0, mine ? g : 0, lane);
-        const int t_end = mine ? min(t1, length_of(s.lengths, v, s.T)) : t0;
-        float k[S];                                                       // dL/dh from behind
+    for (int i = 0; i < S + 2; ++i) { sums[i * kWave] = 0.0; acc[i] = 0.0f; }
+    const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f, d = s.d ? s.d[l.ch] : 0.0f;
+    const int at_place = J * 2 * S / 16 * place_of(lane);                 // the first value a lane has after the exchange, and where it belongs
+    const int to_place = at_place / (2 * S) * 2 * N + at_place % (2 * S) / S * N + q * S + at_place % S;
+    auto last_tile = [&](const Place &p) { return p.t0 + (p.t1 - p.t0 - 1) / K * K; };
+    Place here{slot, 0, 0, 0, 0};
+    bool more = here.settle(s, s.pieces);
+    int t = more ? last_tile(here) : 0, buffer = 0;
+    // the lane's own timesteps: t + 4 i + q
+    float x[R], dt[R], sig[R], gp[R], gz[R], h0[K / kHeld][S], k[S], from_behind[S];
+    BackTile<BF16, S> r;
+    auto take = [&](int steps, float *to) {
+        r.rows.stage(to, lane);
 #pragma unroll
-        for (int i = 0; i < S; ++i) k[i] = 0.0f;
-        if (mine) {
-            if (b.dh_after) load_state(k, b.dh_after + l.state(0));
-            for (int o = s.pieces - 1; o > p; --o) {
-                float there[S];
-                load_state(there, s.piece_state + l.state(o));
-                const float time = s.piece_time[l.channel(o)];
-#pragma unroll
-                for (int i = 0; i < S; ++i) k[i] = fmaf(exp2_of(time * a2[i]), k[i], there[i]);
+        for (int i = 0; i < R; ++i) {
+            x[i] = r.x[i];
+            dt[i] = softplus_of(r.delta[i] + bias, sig[i]);
+            gp[i] = r.gy[i];
+            if (GATE) {
+                const float z = r.z[i], sz = sigmoid_of(z);
+                gz[i] = gp[i] * sz * fmaf(z, 1.0f - sz, 1.0f);
+                gp[i] *= z * sz;
             }
+            if (4 * i + q >= steps) x[i] = dt[i] = gp[i] = 0.0f;
         }
-        for (int t = t0 + (t1 - t0 - 1) / K * K; t >= t0; t -= K, buffer ^= 1) {
-            float *const out = s_bc + (buffer * waves + wave) * V;
-            if (t < t_end) {
-                const int steps = min(K, t_end - t);
-                // the lane's own timesteps: t + 4 i + q
-                float x[R], dt[R], sig[R], gp[R], gz[R], y[R];
 #pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    const bool there = 4 * i + q < steps;
-                    const int64_t at = l.at(t + min(4 * i + q, steps - 1));
-                    x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at);
-                    const float delta = Elem<BF16>::get(static_cast<const E *>(s.delta) + at), gy = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at);
-                    dt[i] = softplus_of(delta + bias, sig[i]);
-                    gp[i] = gy;
-                    gz[i] = 0.0f;
-                    if (s.z) {
-                        const float z = Elem<BF16>::get(static_cast<const E *>(s.z) + at), sz = sigmoid_of(z);
-                        gp[i] = gy * z * sz;
-                        gz[i] = gy * sz * fmaf(z, 1.0f - sz, 1.0f);
-                    }
-                    if (!there) x[i] = dt[i] = gp[i] = 0.0f;
+        for (int i = 0; i < K / kHeld; ++i)
+#pragma unroll
+            for (int m = 0; m < S; ++m) h0[i][m] = r.h[i][m];
+#pragma unroll
+        for (int i = 0; i < S; ++i) from_behind[i] = r.k[i];
+    };
+    if (more) {
+        load_back_tile<BF16, S, GATE>(r, b, l, here, t, min(K, here.t_end - t), true);
+        take(min(K, here.t_end - t), s_mem + wave * V);
+    }
+    while (more) {
+        const int steps = min(K, here.t_end - t);
+        float *const rows = s_mem + buffer * turn + wave * V;
+        const int ahead_buffer = buffer == 2 ? 0 : buffer + 1;
+        Place next = here;
+        int t_next = t - K;
+        if (t_next < here.t0) {
+            next.v += slots;
+            more = next.settle(s, s.pieces);
+            t_next = more ? last_tile(next) : 0;
+        }
+        if (t == last_tile(here))
+#pragma unroll
+            for (int i = 0; i < S; ++i) k[i] = from_behind[i];
+        // The next tile's loads go out now and are taken up behind this one's stores, whose number is known: loads and stores are counted in
+        // one order, and waiting for the loads is waiting until no more than the stores are left.
+        const int steps_next = min(K, next.t_end - t_next);
+        if (more) load_back_tile<BF16, S, GATE>(r, b, l, next, t_next, steps_next, t_next == last_tile(next));
+        const int64_t at = l.at(here.v, t), four = 4 * s.n * s.f;
+        wave_lds_sync();
+        float h[S], held[kHeld][S];
+        auto ahead = [&](auto whole, int i) {         // forward over four timesteps of the tile, their states kept
+            float part_y[4];
+            const float dtx = dt[i] * x[i];
+            auto step = [&](int j, float dt_j, float dtx_j) {
+                const float *const row = rows + (4 * i + j) * 2 * N;
+                float rb[S], rc[S];
+                load_state(rb, row + q * S);
+                if (GATE) load_state(rc, row + N + q * S);
+                float e[S];
+                part_y[j] = 0.0f;
+#pragma unroll
+                for (int m = 0; m < S; ++m) {
+                    held[(4 * i + j) % kHeld][m] = h[m];
+                    e[m] = exp2_of(dt_j * a2[m]);
+                    h[m] = fmaf(e[m], h[m], dtx_j * rb[m]);
+                    if (GATE) part_y[j] = fmaf(rc[m], h[m], part_y[j]);
                 }
-                // forward over the tile, its states kept
-                float h[S], held[K][S];
-                int64_t from = l.state(t / kTile);
-                load_state(h, s.checkpoints + from);
-                auto rows = [&](float (&r)[4][S], int i, int column) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (4 * i + j < steps) Elem<BF16>::template row<S>(r[j], l.b_row(s.bc, t + 4 * i + j) + column);
-                        else
-#pragma unroll
-                            for (int m = 0; m < S; ++m) r[j][m] = 0.0f;
-                    }
-                };
-                auto ahead = [&](float (&h)[S], const float (&row)[S], float dt_j, float dtx_j) {
-#pragma unroll
-                    for (int m = 0; m < S; ++m) h[m] = fmaf(exp2_of(dt_j * a2[m]), h[m], dtx_j * row[m]);
-                };
-                if (K < kTile && (t & (kTile - 1))) {                     // the kept state lies K timesteps back
-                    float dt0[R], dtx0[R], sig0;
-#pragma unroll
-                    for (int i = 0; i < R; ++i) {
-                        const int64_t at = l.at(t - K + 4 * i + q);
-                        dt0[i] = softplus_of(Elem<BF16>::get(static_cast<const E *>(s.delta) + at) + bias, sig0);
-                        dtx0[i] = dt0[i] * Elem<BF16>::get(static_cast<const E *>(s.x) + at);
-                    }
-#pragma unroll
-                    for (int i = 0; i < R; ++i) {
-                        float rb[4][S];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) Elem<BF16>::template row<S>(rb[j], l.b_row(s.bc, t - K + 4 * i + j));
-                        ahead(h, rb[0], of_lane<0>(dt0[i]), of_lane<0>(dtx0[i]));
-                        ahead(h, rb[1], of_lane<1>(dt0[i]), of_lane<1>(dtx0[i]));
-                        ahead(h, rb[2], of_lane<2>(dt0[i]), of_lane<2>(dtx0[i]));
-                        ahead(h, rb[3], of_lane<3>(dt0[i]), of_lane<3>(dtx0[i]));
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    float rb[4][S], rc[4][S], part_y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    rows(rb, i, 0);
-                    if (s.z) rows(rc, i, N);
-                    const float dtx = dt[i] * x[i];
-                    auto step = [&](int j, float dt_j, float dtx_j) {
-#pragma unroll
-                        for (int m = 0; m < S; ++m) held[4 * i + j][m] = h[m];
-                        ahead(h, rb[j], dt_j, dtx_j);
-                        if (s.z)
-#pragma unroll
-                            for (int m = 0; m < S; ++m) part_y[j] = fmaf(rc[j][m], h[m], part_y[j]);
-                    };
-                    step(0, of_lane<0>(dt[i]), of_lane<0>(dtx));
-                    step(1, of_lane<1>(dt[i]), of_lane<1>(dtx));
-                    step(2, of_lane<2>(dt[i]), of_lane<2>(dtx));
-                    step(3, of_lane<3>(dt[i]), of_lane<3>(dtx));
-                    y[i] = fmaf(d, x[i], quad_sums(part_y, q));
-                }
-                // ... and back
-#pragma unroll
-                for (int m = 0; m < S; ++m) acc_a[m] = 0.0f;
-                float acc_d = 0.0f, acc_bias = 0.0f;
-#pragma unroll
-                for (int i = R - 1; i >= 0; --i) {
-                    float rb[4][S], rc[4][S], bc[8 * S], ghb[4], sa[4];
-                    rows(rb, i, 0);
-                    rows(rc, i, N);
-                    const float dtx = dt[i] * x[i];
-                    auto step = [&](int j, float dt_j, float dtx_j, float g_j) {
-                        ghb[j] = sa[j] = 0.0f;
-#pragma unroll
-                        for (int m = 0; m < S; ++m) {
-                            const float gh = fmaf(rc[j][m], g_j, k[m]);
-                            bc[j * 2 * S + m] = gh * dtx_j;
-                            bc[j * 2 * S + S + m] = h[m] * g_j;
-                            ghb[j] = fmaf(gh, rb[j][m], ghb[j]);
-                            h[m] = held[4 * i + j][m];
-                            k[m] = gh * exp2_of(dt_j * a2[m]);
-                            const float u = k[m] * h[m];
-                            sa[j] = fmaf(u, a[m], sa[j]);
-                            acc_a[m] = fmaf(u, dt_j, acc_a[m]);
-                        }
-                    };
-                    step(3, of_lane<3>(dt[i]), of_lane<3>(dtx), of_lane<3>(gp[i]));
-                    step(2, of_lane<2>(dt[i]), of_lane<2>(dtx), of_lane<2>(gp[i]));
-                    step(1, of_lane<1>(dt[i]), of_lane<1>(dtx), of_lane<1>(gp[i]));
-                    step(0, of_lane<0>(dt[i]), of_lane<0>(dtx), of_lane<0>(gp[i]));
-                    const float gb = quad_sums(ghb, q), da = quad_sums(sa, q);
-                    const float ddelta = fmaf(x[i], gb, da) * sig[i];
-                    if (4 * i + q < steps) {
-                        const int64_t at = l.at(t + 4 * i + q);
-                        Elem<BF16>::put(static_cast<E *>(b.dx) + at, fmaf(d, gp[i], dt[i] * gb));
-                        Elem<BF16>::put(static_cast<E *>(b.ddelta) + at, ddelta);
-                        if (s.z) Elem<BF16>::put(static_cast<E *>(b.dz) + at, gz[i] * y[i]);
-                        acc_d = fmaf(gp[i], x[i], acc_d);
-                        acc_bias += ddelta;
-                    }
-                    // value i = step * 2 S + (B or C) * S + state; a lane ends up with 8 S / 16 of them
-                    channel_sums<8 * S>(bc, lane);
-#pragma unroll
-                    for (int m = 0; m < S / 2; ++m) {
-                        const int at = m + (S / 2) * place_of(lane), j = at / (2 * S), rest = at % (2 * S);
-                        out[(4 * i + j) * 2 * N + (rest / S) * N + q * S + rest % S] = bc[m];
-                    }
-                }
-#pragma unroll
-                for (int m = 0; m < S; ++m) sum_a[m] += (double)acc_a[m];
-                sum_d += (double)acc_d;
-                sum_bias += (double)acc_bias;
-            } else
-                for (int i = lane; i < V; i += kWave) out[i] = 0.0f;
-            if (mine)
-                for (int o = max(t, t_end) + q; o < min(t + K, t1); o += 4) {
-                    const int64_t at = l.at(o);
-                    Elem<BF16>::put(static_cast<E *>(b.dx) + at, 0.0f);
-                    Elem<BF16>::put(static_cast<E *>(b.ddelta) + at, 0.0f);
-                    if (s.z) Elem<BF16>::put(static_cast<E *>(b.dz) + at, 0.0f);
-                }
-            __syncthreads();                                              // two buffers: the next tile's values do not meet this one's readers
-            const float *const all = s_bc + buffer * waves * V;
-            for (int i = threadIdx.x; i < b.sequences * V; i += blockDim.x) {
-                const int r = i / V, e = i % V, j = e / (2 * N), column = e % (2 * N);
-                float sum = all[r * own * V + e];
-                for (int w = 1; w < own; ++w) sum += all[(r * own + w) * V + e];
-                if (first + r < s.n && t + j < t1) {
-                    const int64_t at = ((int64_t)(t + j) * s.n + first + r) * 2 * N + column;
-                    if (b.dbc_part) b.dbc_part[(int64_t)part * s.T * s.n * 2 * N + at] = sum;
-                    else Elem<BF16>::put(static_cast<E *>(b.dbc) + at, sum);
-                }
+                if (kDecays<S>) store_state(decays + (4 * i + j) % kHeld * kWave * S, e);
+            };
+            step(0, of_lane<0>(dt[i]), of_lane<0>(dtx));
+            step(1, of_lane<1>(dt[i]), of_lane<1>(dtx));
+            step(2, of_lane<2>(dt[i]), of_lane<2>(dtx));
+            step(3, of_lane<3>(dt[i]), of_lane<3>(dtx));
+            if (GATE) {
+                const float dz = gz[i] * fmaf(d, x[i], quad_sums(part_y, q));
+                if (decltype(whole)::value || 4 * i + q < steps) Elem<BF16>::put(static_cast<E *>(b.dz) + at + i * four, dz);
             }
-        }
-        if (mine && b.dh_before && p == 0) store_state(b.dh_before + l.state(0), k);
-    }
-    // sums over time and sequences: one place per workgroup and sequence beside others
-    if (in_width) {
-        double *to = b.sums + ((int64_t)slot * b.sequences + which) * s.f * (N + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto back = [&](auto whole, int i) {          // ... and back over them
+            float bc[J * 2 * S], ghb[4], sa[4];
+            const float dtx = dt[i] * x[i];
+            auto step = [&](int j, float dt_j, float dtx_j, float g_j) {
+                const float *const row = rows + (4 * i + j) * 2 * N;
+                float rb[S], rc[S];
+                load_state(rb, row + q * S);
+                load_state(rc, row + N + q * S);
+                float e[S];
+                if (kDecays<S>) load_state(e, decays + (4 * i + j) % kHeld * kWave * S);
+                ghb[j] = sa[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S; ++i) to[(int64_t)ch * N + q * S + i] = sum_a[i];
-        sum_d += __shfl_xor(sum_d, 1);
-        sum_d += __shfl_xor(sum_d, 2);
-        sum_bias += __shfl_xor(sum_bias, 1);
-        sum_bias += __shfl_xor(sum_bias, 2);
-        if (q == 0) { to[(int64_t)s.f * N + ch] = sum_d; to[(int64_t)s.f * (N + 1) + ch] = sum_bias; }
+                for (int m = 0; m < S; ++m) {
+                    const float gh = fmaf(rc[m], g_j, k[m]);
+                    bc[j % J * 2 * S + m] = gh * dtx_j;
+                    bc[j % J * 2 * S + S + m] = h[m] * g_j;
+                    ghb[j] = fmaf(gh, rb[m], ghb[j]);
+                    h[m] = held[(4 * i + j) % kHeld][m];
+                    k[m] = gh * (kDecays<S> ? e[m] : exp2_of(dt_j * a2[m]));
+                    const float u = k[m] * h[m];
+                    sa[j] = fmaf(u, a2[m], sa[j]);
+                    acc[m] = fmaf(u, dt_j, acc[m]);
+                }
+            };
+            // value v of the exchange = step * 2 S + (B or C) * S + state; a lane ends up with J 2 S / 16 of them
+            auto leave = [&](int j0) {
+                channel_sums<J * 2 * S>(bc, lane);
+#pragma unroll
+                for (int m = 0; m < J * 2 * S / 16; ++m) rows[(4 * i + j0) * 2 * N + to_place + m] = bc[m];
+            };
+            step(3, of_lane<3>(dt[i]), of_lane<3>(dtx), of_lane<3>(gp[i]));
+            step(2, of_lane<2>(dt[i]), of_lane<2>(dtx), of_lane<2>(gp[i]));
+            if (J == 2) leave(2);
+            step(1, of_lane<1>(dt[i]), of_lane<1>(dtx), of_lane<1>(gp[i]));
+            step(0, of_lane<0>(dt[i]), of_lane<0>(dtx), of_lane<0>(gp[i]));
+            leave(0);
+            const float gb = quad_sums(ghb, q), da = quad_sums(sa, q) * kLn2;
+            const float ddelta = fmaf(x[i], gb, da) * sig[i];
+            if (decltype(whole)::value || 4 * i + q < steps) {
+                Elem<BF16>::put(static_cast<E *>(b.dx) + at + i * four, fmaf(d, gp[i], dt[i] * gb));
+                Elem<BF16>::put(static_cast<E *>(b.ddelta) + at + i * four, ddelta);
+                acc[S] = fmaf(gp[i], x[i], acc[S]);
+                acc[S + 1] += ddelta;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto start = [&](int half) {
+#pragma unroll
+            for (int m = 0; m < S; ++m) h[m] = h0[half][m];
+        };
+        if (steps == K) {
+            const std::true_type whole;
+            start(K / kHeld - 1);
+            ahead(whole, R - 2);
+            ahead(whole, R - 1);
+            back(whole, R - 1);
+            back(whole, R - 2);
+            if (K > kHeld) {
+                start(0);
+                ahead(whole, 0);
+                ahead(whole, 1);
+                back(whole, 1);
+                back(whole, 0);
+            }
+            if (more) take(steps_next, s_mem + ahead_buffer * turn + wave * V);
+        } else {                          // fours of which nothing is there are left out; what is missing of the last one is zero
+            const std::false_type whole;
+#pragma unroll
+            for (int half = K / kHeld - 1; half >= 0; --half)
+                if (half * kHeld < steps) {
+                    start(half);
+                    ahead(whole, 2 * half);
+                    if (half * kHeld + 4 < steps) {
+                        ahead(whole, 2 * half + 1);
+                        back(whole, 2 * half + 1);
+                    }
+                    back(whole, 2 * half);
+                }
+            for (int o = max(steps, 0); o < K; o += 4)
+                if (o + q < K && t + o + q < here.t1) {
+                    const int64_t to = l.at(here.v, t + o);
+                    Elem<BF16>::put(static_cast<E *>(b.dx) + to, 0.0f);
+                    Elem<BF16>::put(static_cast<E *>(b.ddelta) + to, 0.0f);
+                    if (GATE) Elem<BF16>::put(static_cast<E *>(b.dz) + to, 0.0f);
+                }
+            if (more) take(steps_next, s_mem + ahead_buffer * turn + wave * V);
+        }
+        if ((t & 63) == 0 || t == here.t0)
+#pragma unroll
+            for (int i = 0; i < S + 2; ++i) { sums[i * kWave] += (double)acc[i]; acc[i] = 0.0f; }
+        block_lds_sync();
+        const float *const all = s_mem + buffer * turn;
+        for (int i = threadIdx.x; i < V; i += active * kWave) {
+            const int j = i / (2 * N), column = i % (2 * N);
+            if (t + j >= here.t1) break;
+            float sum = 0.0f;
+            if (j < steps)
+                for (int o = 0; o < active; ++o) sum += all[o * V + i];
+            const int64_t to = ((int64_t)(t + j) * s.n + here.v) * 2 * N + column;
+            if (b.dbc_part) b.dbc_part[(int64_t)part * s.T * s.n * 2 * N + to] = sum;
+            else Elem<BF16>::put(static_cast<E *>(b.dbc) + to, sum);
+        }
+        if (b.dh_before && here.p == 0 && t == here.t0) store_state(b.dh_before + l.state(0, here.v), k);
+        buffer = ahead_buffer;
+        here = next;
+        t = t_next;
     }
+    // sums over time and sequences
+    double *to = b.sums + (int64_t)slot * s.f * (N + 2);
+#pragma unroll
+    for (int i = 0; i < S; ++i) to[(int64_t)l.ch * N + q * S + i] = sums[i * kWave];
+    double sum_d = sums[S * kWave], sum_bias = sums[(S + 1) * kWave];
+    sum_d += __shfl_xor(sum_d, 1);
+    sum_d += __shfl_xor(sum_d, 2);
+    sum_bias += __shfl_xor(sum_bias, 1);
+    sum_bias += __shfl_xor(sum_bias, 2);
+    if (q == 0) { to[(int64_t)s.f * N + l.ch] = sum_d; to[(int64_t)s.f * (N + 1) + l.ch] = sum_bias; }
 }
 
-// da | dd | ddt_bias from the workgroups' sums, sixteen at a time and in a fixed order.
-__global__ __launch_bounds__(256) void scan_sums_kernel(const double *__restrict__ sums, int slots, int states, int rest, float *__restrict__ da, float *__restrict__ dd,
-                                                        float *__restrict__ ddt_bias, int accumulate) {
-    __shared__ double s_part[16][17];
+// da | dd | ddt_bias from the workgroups' sums, 64 strided parts of them added up in a fixed order.
+__global__ __launch_bounds__(1024) void scan_sums_kernel(const double *__restrict__ sums, int slots, int states, int rest, float *__restrict__ da, float *__restrict__ dd,
+                                                         float *__restrict__ ddt_bias, int accumulate) {
+    __shared__ double s_part[64][17];
     const int o = threadIdx.x % 16, r = threadIdx.x / 16, at = blockIdx.x * 16 + o, width = states + 2 * rest;
     double sum = 0.0;
     if (at < width)
-        for (int k = r; k < slots; k += 16) sum += sums[(int64_t)k * width + at];
+#pragma unroll 4
+        for (int k = r; k < slots; k += 64) sum += sums[(int64_t)k * width + at];
     s_part[r][o] = sum;
     __syncthreads();
     if (r == 0 && at < width) {
-        for (int k = 1; k < 16; ++k) sum += s_part[k][o];
+#pragma unroll 7
+        for (int k = 1; k < 64; ++k) sum += s_part[k][o];
         float *to = at < states ? da + at : at < states + rest ? (dd ? dd + (at - states) : nullptr) : ddt_bias ? ddt_bias + (at - states - rest) : nullptr;
         if (to) *to = accumulate ? (float)((double)*to + sum) : (float)sum;
     }
@@ -656,17 +805,16 @@ Pieces pieces_of(int64_t T, int64_t items, int64_t wanted) {
 
 Pieces forward_pieces(int64_t T, int64_t n, int32_t f) { return pieces_of(T, n * (f / kChannels), 4096); }
 
-struct BackShape { int groups, blocks_of_groups, sequences, waves; int64_t rows; Pieces pieces; int64_t slots; };
+struct BackShape { int groups, blocks_of_groups, waves; Pieces pieces; int64_t slots; };
 
 BackShape back_shape(int64_t T, int64_t n, int32_t f) {
     BackShape b;
     b.groups = f / kChannels;
     b.blocks_of_groups = (b.groups + kBackWaves - 1) / kBackWaves;
-    b.sequences = b.groups < kBackWaves ? kBackWaves / b.groups : 1;
-    b.waves = b.blocks_of_groups > 1 ? kBackWaves : b.sequences * b.groups;
-    b.rows = (n + b.sequences - 1) / b.sequences;
-    b.pieces = pieces_of(T, b.rows * b.blocks_of_groups, 512);
-    b.slots = std::max<int64_t>(1, std::min<int64_t>(b.rows * b.pieces.count, kMaxSlots / 2 / b.blocks_of_groups));
+    b.waves = std::min(b.groups, kBackWaves);
+    const int64_t blocks = std::max(1, kBackResident / (b.waves * b.blocks_of_groups));
+    b.pieces = pieces_of(T, n, blocks);
+    b.slots = std::min<int64_t>(n * b.pieces.count, blocks);
     return b;
 }
 
@@ -684,8 +832,11 @@ void place_pieces(Scan &s, const Pieces &p, int32_t N, void *ws) {
     }
 }
 
-dim3 walk_grid(const Scan &s, int pieces) {
-    return dim3((unsigned)std::min<int64_t>((s.n * s.groups + kWaves - 1) / kWaves, std::max(1, kMaxGrid / pieces)), (unsigned)pieces);
+// Wavefronts that stay: as many workgroups as the device holds, or as there is work for.  All channels of a sequence have one (there are
+// at most 1024 groups of them, and never fewer than 256 workgroups at once).
+template <typename K> dim3 walk_grid(K kernel, const Scan &s, int pieces) {
+    const int64_t work = (s.n * s.groups * pieces + kWaves - 1) / kWaves;
+    return dim3((unsigned)std::min<int64_t>(work, std::max<int64_t>(DGNN_MAX_CHANNELS / kChannels / kWaves, resident_workgroups(kernel, kWaves * kWave, 1024))));
 }
 
 // kernel<BF16, S> by storage type and state size
@@ -708,7 +859,7 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 extern "C" int dgnn_selective_scan_checkpoints(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes) {
     if (!bytes) return DGNN_ERR_NULL;
     if (int rc = check_shape(T, n, f, states)) return rc;
-    *bytes = (size_t)((T + kTile - 1) / kTile) * n * f * states * sizeof(float);
+    *bytes = (size_t)((T + kHeld - 1) / kHeld) * n * f * states * sizeof(float);
     return DGNN_OK;
 }
 
@@ -728,7 +879,7 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
     for (const void *p : {x, delta, bc, z, (const void *)h_before, (const void *)y, (const void *)h_after, (const void *)checkpoints, (const void *)ws})
         if (p && !aligned16(p)) return DGNN_ERR_ALIGN;
     const size_t frame = (size_t)T * n * f * (dt == DGNN_F32 ? 4 : 2), rows = (size_t)T * n * 2 * states * (dt == DGNN_F32 ? 4 : 2);
-    const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kTile - 1) / kTile) * state;
+    const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kHeld - 1) / kHeld) * state;
     for (auto o : {std::pair<const void *, size_t>{y, frame}, {h_after, state}, {checkpoints, kept}, {ws, ws_bytes}}) {
         for (auto i : {std::pair<const void *, size_t>{x, frame}, {delta, frame}, {bc, rows}, {z, frame}})
             if (overlap(o.first, o.second, i.first, i.second)) return DGNN_ERR_ALIAS;
@@ -744,12 +895,18 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
     hipStream_t st = (hipStream_t)stream;
     if (s.pieces > 1) {
         const int rc = by_kind(dt, states, [&](auto bf16, auto per) {
-            hipLaunchKernelGGL((scan_piece_kernel<decltype(bf16)::value, decltype(per)::value>), walk_grid(s, s.pieces - 1), dim3(kWaves * kWave), 0, st, s);
+            const auto kernel = scan_piece_kernel<decltype(bf16)::value, decltype(per)::value>;
+            hipLaunchKernelGGL(kernel, walk_grid(kernel, s, s.pieces - 1), dim3(kWaves * kWave), 0, st, s);
         });
         if (rc) return rc;
+        if (s.pieces > 2) {
+            hipLaunchKernelGGL(join_kernel<1>, dim3((unsigned)((n * f * states + 255) / 256)), dim3(256), 0, st, s, (const float *)nullptr, states);
+            DGNN_RETURN_IF_LAUNCH_FAILED();
+        }
     }
     return by_kind(dt, states, [&](auto bf16, auto per) {
-        hipLaunchKernelGGL((scan_kernel<decltype(bf16)::value, decltype(per)::value>), walk_grid(s, s.pieces), dim3(kWaves * kWave), 0, st, s);
+        const auto kernel = z ? scan_kernel<decltype(bf16)::value, decltype(per)::value, true> : scan_kernel<decltype(bf16)::value, decltype(per)::value, false>;
+        hipLaunchKernelGGL(kernel, walk_grid(kernel, s, s.pieces), dim3(kWaves * kWave), 0, st, s);
     });
 }
 
@@ -757,7 +914,7 @@ extern "C" int dgnn_selective_scan_backward_workspace(int64_t T, int64_t n, int3
     if (!bytes) return DGNN_ERR_NULL;
     if (int rc = check_shape(T, n, f, states)) return rc;
     const BackShape b = back_shape(T, n, f);
-    *bytes = piece_bytes(b.pieces, n, f, states) + round_up((size_t)b.slots * b.sequences * f * (states + 2) * sizeof(double), 256) +
+    *bytes = piece_bytes(b.pieces, n, f, states) + round_up((size_t)b.slots * f * (states + 2) * sizeof(double), 256) +
              (b.blocks_of_groups > 1 ? (size_t)b.blocks_of_groups * T * n * 2 * states * sizeof(float) : 0);
     return DGNN_OK;
 }
@@ -778,7 +935,7 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
     dgnn_selective_scan_backward_workspace(T, n, f, states, &need);
     if (ws_bytes < need) return DGNN_ERR_CAPACITY;
     const size_t frame = (size_t)T * n * f * (dt == DGNN_F32 ? 4 : 2), rows = (size_t)T * n * 2 * states * (dt == DGNN_F32 ? 4 : 2);
-    const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kTile - 1) / kTile) * state;
+    const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kHeld - 1) / kHeld) * state;
     const std::pair<const void *, size_t> in[] = {{x, frame}, {delta, frame}, {bc, rows}, {z, frame}, {checkpoints, kept}, {g_y, frame}, {dh_after, state}};
     const std::pair<const void *, size_t> out[] = {{dx, frame}, {ddelta, frame}, {dbc, rows}, {dz, frame}, {dh_before, state}, {ws, ws_bytes}};
     for (size_t i = 0; i < sizeof(out) / sizeof(*out); ++i) {
@@ -793,31 +950,34 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
     place_pieces(b.s, shape.pieces, states, ws);
     b.g_y = g_y; b.dh_after = dh_after; b.dx = dx; b.ddelta = ddelta; b.dbc = dbc; b.dz = dz; b.dh_before = dh_before;
     b.blocks_of_groups = shape.blocks_of_groups;
-    b.sequences = shape.sequences;
     char *at = static_cast<char *>(ws) + piece_bytes(shape.pieces, n, f, states);
     b.sums = reinterpret_cast<double *>(at);
-    at += round_up((size_t)shape.slots * shape.sequences * f * (states + 2) * sizeof(double), 256);
+    at += round_up((size_t)shape.slots * f * (states + 2) * sizeof(double), 256);
     b.dbc_part = shape.blocks_of_groups > 1 ? reinterpret_cast<float *>(at) : nullptr;
     hipStream_t st = (hipStream_t)stream;
     if (b.s.pieces > 1) {
         const int rc = by_kind(dt, states, [&](auto bf16, auto per) {
-            hipLaunchKernelGGL((scan_back_piece_kernel<decltype(bf16)::value, decltype(per)::value>), walk_grid(b.s, b.s.pieces - 1), dim3(kWaves * kWave), 0, st, b);
+            const auto kernel = scan_back_piece_kernel<decltype(bf16)::value, decltype(per)::value>;
+            hipLaunchKernelGGL(kernel, walk_grid(kernel, b.s, b.s.pieces - 1), dim3(kWaves * kWave), 0, st, b);
         });
         if (rc) return rc;
+        hipLaunchKernelGGL(join_kernel<-1>, dim3((unsigned)((n * f * states + 255) / 256)), dim3(256), 0, st, b.s, dh_after, states);
+        DGNN_RETURN_IF_LAUNCH_FAILED();
     }
     int rc = by_kind(dt, states, [&](auto bf16, auto per) {
         constexpr int S = decltype(per)::value;
-        const unsigned lds = 2u * shape.waves * kHeld<S> * 8 * S * sizeof(float);
-        hipLaunchKernelGGL((scan_back_kernel<decltype(bf16)::value, S>), dim3((unsigned)(shape.slots * shape.blocks_of_groups)), dim3(shape.waves * kWave), lds, st, b);
+        const unsigned lds = shape.waves * ((3u * kBackTile<S> * 8 * S + kDecays<S> * kWave) * sizeof(float) + (S + 2) * kWave * sizeof(double));
+        const auto kernel = z ? scan_back_kernel<decltype(bf16)::value, S, true> : scan_back_kernel<decltype(bf16)::value, S, false>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(shape.slots * shape.blocks_of_groups)), dim3(shape.waves * kWave), lds, st, b);
     });
     if (rc) return rc;
     const int width = f * (states + 2);
-    hipLaunchKernelGGL(scan_sums_kernel, dim3((unsigned)((width + 15) / 16)), dim3(256), 0, st, b.sums, (int)(shape.slots * shape.sequences), f * states, f, da, dd, ddt_bias,
+    hipLaunchKernelGGL(scan_sums_kernel, dim3((unsigned)((width + 15) / 16)), dim3(1024), 0, st, b.sums, (int)shape.slots, f * states, f, da, dd, ddt_bias,
                        accumulate);
     DGNN_RETURN_IF_LAUNCH_FAILED();
     if (b.dbc_part) {
         const int64_t count = T * n * 2 * states;
-        const unsigned blocks = (unsigned)std::min<int64_t>((count + 255) / 256, kMaxGrid);
+        const unsigned blocks = (unsigned)std::min<int64_t>((count + 255) / 256, 1 << 20);
         if (dt == DGNN_BF16) hipLaunchKernelGGL(scan_rows_kernel<true>, dim3(blocks), dim3(256), 0, st, b.dbc_part, shape.blocks_of_groups, count, dbc);
         else hipLaunchKernelGGL(scan_rows_kernel<false>, dim3(blocks), dim3(256), 0, st, b.dbc_part, shape.blocks_of_groups, count, dbc);
         DGNN_RETURN_IF_LAUNCH_FAILED();

@@ -83,7 +83,7 @@ def test_scan_refusals(lib):
     rc, long_need = size(lib.dgnn_selective_scan_workspace, 4096, 1, 32, 16)
     assert rc == 0 and long_need > need
     assert call(T=4096, n=1, wsb=long_need - 1) == CAPACITY
-    assert size(lib.dgnn_selective_scan_checkpoints, 33, 8, 32, 16) == (0, 3 * 8 * 32 * 16 * 4)
+    assert size(lib.dgnn_selective_scan_checkpoints, 33, 8, 32, 16) == (0, 5 * 8 * 32 * 16 * 4)
     assert size(lib.dgnn_selective_scan_checkpoints, 33, 8, 32, 4)[0] == SHAPE and lib.dgnn_selective_scan_checkpoints(33, 8, 32, 16, None) == NULL
 
 
@@ -170,4 +170,4 @@ def test_binding_refuses():
         dg.Gradients([])
     with pytest.raises(ValueError):
         dg.Gradients([torch.zeros(3)])
-    assert binding.selective_scan_checkpoints(17, 2, 16, 8) == 2 * 2 * 16 * 8
+    assert binding.selective_scan_checkpoints(17, 2, 16, 8) == 3 * 2 * 16 * 8
