@@ -33,6 +33,7 @@ constexpr int kTile = 16;                 // timesteps of a tile
 constexpr int kHeld = 8;                  // ... between two kept states: the adjoint holds the states of so many in registers
 constexpr int kWaves = 4;                 // wavefronts of a workgroup of the kernels without sums over channels
 constexpr int kBackWaves = 8;             // ... of the adjoint, at most
+constexpr int kMaxGrid = 1 << 22;         // workgroups of a launch: HIP counts its threads in 32 bits
 constexpr int kBackResident = 2048;       // ... of all its workgroups: two on a SIMD
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;
@@ -202,8 +203,13 @@ template <int S> struct Lane {
 
 // a log2(e) of a lane's states: e = 2^(dt a2).
 template <int S> __device__ __forceinline__ void load_decay(float (&a2)[S], const float *a, int ch, int q) {
+    const float *const p = a + (int64_t)ch * 4 * S + q * S;
+    if ((reinterpret_cast<uintptr_t>(a) & 15) == 0) load_state(a2, p);            // a needs the alignment of a float only
+    else
 #pragma unroll
-    for (int s = 0; s < S; ++s) a2[s] = a[(int64_t)ch * 4 * S + q * S + s] * kLog2e;
+        for (int s = 0; s < S; ++s) a2[s] = p[s];
+#pragma unroll
+    for (int s = 0; s < S; ++s) a2[s] *= kLog2e;
 }
 
 // Sequence v in piece p of the time axis: timesteps [t0, t1), of which the sequence has those ahead of t_end.
@@ -412,6 +418,51 @@ template <bool BF16, int S> __global__ __launch_bounds__(kWaves *kWave) void sca
     scan_tiles<BF16, S, false, false>(s, s_rows);
 }
 
+// One timestep, the step of a model that follows a running series: a wavefront per sixteen channels of a sequence and no more.  The state
+// comes and goes (8 N bytes a channel against 4 x 2 or 4 of everything else), and what streams it is many wavefronts that are soon done.
+template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWave) void scan_step_kernel(Scan s) {
+    typedef typename Elem<BF16>::Type E;
+    constexpr int N = 4 * S;
+    const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
+    for (int64_t i = (int64_t)blockIdx.x * kWaves + wave; i < s.n * s.groups; i += (int64_t)gridDim.x * kWaves) {
+        const bool narrow = i >> 32 == 0;
+        const int64_t v = narrow ? (uint32_t)i / (uint32_t)s.groups : i / s.groups;
+        const Lane<S> l(s, (int)(i - v * s.groups), lane);
+        const int64_t at = v * s.f + l.ch;
+        float h[S], a2[S], b[S], c[S];
+        if (s.h_before) load_state(h, s.h_before + l.state(0, v));
+        else
+#pragma unroll
+            for (int k = 0; k < S; ++k) h[k] = 0.0f;
+        if (length_of(s.lengths, v, 1) == 0) {
+            if (l.q == 0) Elem<BF16>::put(static_cast<E *>(s.y) + at, 0.0f);
+            if (s.h_after) store_state(s.h_after + l.state(0, v), h);
+            continue;
+        }
+        const E *const row = static_cast<const E *>(s.bc) + v * 2 * N + l.q * S;
+        Elem<BF16>::template row<S>(b, row);
+        Elem<BF16>::template row<S>(c, row + N);
+        const float x = Elem<BF16>::get(static_cast<const E *>(s.x) + at), delta = Elem<BF16>::get(static_cast<const E *>(s.delta) + at);
+        const float z = GATE ? Elem<BF16>::get(static_cast<const E *>(s.z) + at) : 0.0f;
+        load_decay(a2, s.a, l.ch, l.q);
+        if (s.checkpoints) store_state(s.checkpoints + l.state(0, v), h);
+        float sig, y = 0.0f;
+        const float dt = softplus_of(delta + (s.dt_bias ? s.dt_bias[l.ch] : 0.0f), sig), dtx = dt * x;
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+            h[k] = fmaf(exp2_of(dt * a2[k]), h[k], dtx * b[k]);
+            y = fmaf(c[k], h[k], y);
+        }
+        // the sum in the order of quad_sums, so that a series taken step by step gives the same bits
+        y += dpp<0x4e>(y);
+        y += dpp<0xb1>(y);
+        y = fmaf(s.d ? s.d[l.ch] : 0.0f, x, y);
+        if (GATE) y *= z * sigmoid_of(z);
+        if (s.h_after) store_state(s.h_after + l.state(0, v), h);
+        if (l.q == 0) Elem<BF16>::put(static_cast<E *>(s.y) + at, y);
+    }
+}
+
 // The states between the pieces, in place.  Forward (STEP 1): piece p left part[p] behind when it started from zero, part[0] from h_before;
 // the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
 // reaches piece p from behind takes the place p + 1.  A lane has one state and fetches kJoin pieces' parts together.
@@ -445,44 +496,68 @@ template <int STEP> __global__ __launch_bounds__(256) void join_kernel(Scan s, c
 template <bool BF16, int S>
 __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
-    constexpr int N = 4 * S;
+    constexpr int N = 4 * S, R = kTile / 4;
+    __shared__ float s_rows[kWaves * kTile * 2 * N];
     const Scan &s = b.s;
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
     const int w = blockIdx.x * kWaves + wave, stride = (int)(gridDim.x * kWaves) / s.groups;
     if (w / s.groups >= stride) return;
+    float *const rows = s_rows + wave * kTile * 2 * N;
     const Lane<S> l(s, w % s.groups, lane);
     const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f;
     float a2[S];
     load_decay(a2, s.a, l.ch, l.q);
     for (Place here{w / s.groups, 1, 0, 0, 0}; here.settle(s, s.pieces); here.v += stride) {
-        float k[S], time = 0.0f;
+        Rows<BF16, S, kTile> bc;
+        float k[S], time = 0.0f, delta[R], gy[R], z[R];
 #pragma unroll
         for (int i = 0; i < S; ++i) k[i] = 0.0f;
-        auto four = [&](int t, int steps) {
-            const bool there = l.q < steps;
-            const int64_t at = l.at(here.v, t) - (there ? 0 : (int64_t)(l.q - (steps - 1)) * s.n * s.f);
-            float sig, gy = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at);
-            if (s.z) {
-                const float z = Elem<BF16>::get(static_cast<const E *>(s.z) + at);
-                gy *= z * sigmoid_of(z);
-            }
-            const float dt = softplus_of(Elem<BF16>::get(static_cast<const E *>(s.delta) + at) + bias, sig);
-            time += there ? dt : 0.0f;
-            auto step = [&](float dt_j, float g_j, int j) {
-                float c[S];
-                Elem<BF16>::template row<S>(c, static_cast<const E *>(s.bc) + (((int64_t)(t + j) * s.n + here.v) * 2 + 1) * N + l.q * S);
+        auto load = [&](int t) {
+            const int steps = here.t_end - t;
+            bc.load(s.bc, s.n, here.v, t, steps, lane);
+            const int64_t at = l.at(here.v, t), four = 4 * s.n * s.f;
 #pragma unroll
-                for (int m = 0; m < S; ++m) k[m] = exp2_of(dt_j * a2[m]) * fmaf(c[m], g_j, k[m]);
-            };
-            if (steps > 3) step(of_lane<3>(dt), of_lane<3>(gy), 3);
-            if (steps > 2) step(of_lane<2>(dt), of_lane<2>(gy), 2);
-            if (steps > 1) step(of_lane<1>(dt), of_lane<1>(gy), 1);
-            step(of_lane<0>(dt), of_lane<0>(gy), 0);
+            for (int i = 0; i < R; ++i)
+                if (4 * i + l.q < steps) {
+                    delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at + i * four);
+                    gy[i] = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at + i * four);
+                    if (s.z) z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at + i * four);
+                }
         };
-        if (here.t_end > here.t0) {
-            int t = here.t0 + ((here.t_end - here.t0 - 1) & ~3);
-            if (here.t_end - t < 4) { four(t, here.t_end - t); t -= 4; }
-            for (; t >= here.t0; t -= 4) four(t, 4);
+        int t = here.t0 + (here.t_end - here.t0 - 1) / kTile * kTile;
+        if (here.t_end > here.t0) load(t);
+        else t = here.t0 - 1;
+        for (; t >= here.t0; t -= kTile) {
+            const int steps = min(kTile, here.t_end - t);
+            float dt[R], g[R];
+            bc.stage(rows, lane);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float sig;
+                dt[i] = softplus_of(delta[i] + bias, sig);
+                g[i] = gy[i];
+                if (s.z) g[i] *= z[i] * sigmoid_of(z[i]);
+                if (4 * i + l.q >= steps) dt[i] = g[i] = 0.0f;            // decay 1, nothing added: rows behind the sequence are zero
+                time += dt[i];
+            }
+            wave_lds_sync();
+            if (t > here.t0) load(t - kTile);
+            auto four = [&](int i) {
+                auto step = [&](int j, float dt_j, float g_j) {
+                    float c[S];
+                    load_state(c, rows + (4 * i + j) * 2 * N + N + l.q * S);
+#pragma unroll
+                    for (int m = 0; m < S; ++m) k[m] = exp2_of(dt_j * a2[m]) * fmaf(c[m], g_j, k[m]);
+                };
+                step(3, of_lane<3>(dt[i]), of_lane<3>(g[i]));
+                step(2, of_lane<2>(dt[i]), of_lane<2>(g[i]));
+                step(1, of_lane<1>(dt[i]), of_lane<1>(g[i]));
+                step(0, of_lane<0>(dt[i]), of_lane<0>(g[i]));
+            };
+#pragma unroll
+            for (int i = R - 1; i >= 0; --i)
+                if (4 * i < steps) four(i);
+            wave_lds_sync();
         }
         time = quad_sum(time);
         store_state(s.piece_state + l.state(here.p, here.v), k);
@@ -904,6 +979,11 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
             DGNN_RETURN_IF_LAUNCH_FAILED();
         }
     }
+    if (T == 1)
+        return by_kind(dt, states, [&](auto bf16, auto per) {
+            const auto kernel = z ? scan_step_kernel<decltype(bf16)::value, decltype(per)::value, true> : scan_step_kernel<decltype(bf16)::value, decltype(per)::value, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((n * s.groups + kWaves - 1) / kWaves, kMaxGrid)), dim3(kWaves * kWave), 0, st, s);
+        });
     return by_kind(dt, states, [&](auto bf16, auto per) {
         const auto kernel = z ? scan_kernel<decltype(bf16)::value, decltype(per)::value, true> : scan_kernel<decltype(bf16)::value, decltype(per)::value, false>;
         hipLaunchKernelGGL(kernel, walk_grid(kernel, s, s.pieces), dim3(kWaves * kWave), 0, st, s);
