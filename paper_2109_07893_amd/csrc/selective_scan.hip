@@ -185,7 +185,7 @@ template <int S> __device__ __forceinline__ void store_state(float *p, const flo
 }
 
 __device__ __forceinline__ int length_of(const int32_t *lengths, int64_t v, int T) {
-    return lengths ? min(max(uniform(lengths[v]), 0), T) : T;
+    return lengths ? min(max(as_constant(lengths)[v], 0), T) : T;
 }
 
 // What a wavefront's lane is: its channel, its quarter of the states, and where its values lie in the frames.
@@ -241,13 +241,22 @@ template <bool BF16, int S, int K> struct Rows {
             if (row < steps) r[i] = p[(int64_t)row * n * kRow + at % kRow];
         }
     }
-    __device__ __forceinline__ void stage(float *to, int lane) const {
+    // The same without a branch: rows behind the sequence are fetched from the last one's place and left out of the stage.
+    __device__ __forceinline__ void load_all(const void *bc, int64_t n, int64_t v, int t, int steps, int lane) {
+        const uintx4 *const p = static_cast<const uintx4 *>(bc) + ((int64_t)t * n + v) * kRow;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = i * kWave + lane;
+            r[i] = p[min(at / kRow, steps - 1) * (n * kRow) + at % kRow];
+        }
+    }
+    template <bool ALL> __device__ __forceinline__ void stage(float *to, int lane, int steps) const {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int at = i * kWave + lane;
             if (kPieces % kWave == 0 || at < kPieces) {
                 float v[kValues];
-                Pack<BF16>::unpack(v, r[i]);
+                Pack<BF16>::unpack(v, !ALL || at / kRow < steps ? r[i] : uintx4{0, 0, 0, 0});
 #pragma unroll
                 for (int k = 0; k < kValues; k += 4) *reinterpret_cast<uintx4 *>(to + at * kValues + k) = Pack<false>::pack({v[k], v[k + 1], v[k + 2], v[k + 3]});
             }
@@ -316,7 +325,7 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
     Tile<BF16, S> r;
     float x[kTile / 4], z[kTile / 4], dt[kTile / 4], start[S];
     auto take = [&](int steps, int to) {
-        r.rows.stage(rows + to * kTile * 2 * N, lane);
+        r.rows.template stage<false>(rows + to * kTile * 2 * N, lane, steps);
 #pragma unroll
         for (int i = 0; i < kTile / 4; ++i)
             if (4 * i < steps) {
@@ -466,7 +475,7 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
 // The states between the pieces, in place.  Forward (STEP 1): piece p left part[p] behind when it started from zero, part[0] from h_before;
 // the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
 // reaches piece p from behind takes the place p + 1.  A lane has one state and fetches kJoin pieces' parts together.
-constexpr int kJoin = 16;
+constexpr int kJoin = 32;
 template <int STEP> __global__ __launch_bounds__(256) void join_kernel(Scan s, const float *behind, int states) {
     const int64_t width = s.n * s.f * states, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= width) return;
@@ -530,7 +539,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
         for (; t >= here.t0; t -= kTile) {
             const int steps = min(kTile, here.t_end - t);
             float dt[R], g[R];
-            bc.stage(rows, lane);
+            bc.template stage<false>(rows, lane, steps);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 float sig;
@@ -567,6 +576,10 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
 
 // Timesteps of a tile of the adjoint: what a wavefront fetches ahead.
 template <int S> constexpr int kBackTile = S <= 4 ? 16 : 8;
+// Whether a tile's loads are all made, whatever is there of it.  With 32 states, where the registers are short, the loads that a branch may
+// pass over cost more (2^17 x 128 fp32: 922 us against 658); with 16 and 8 the addresses that take the branches' place do (338 against 382,
+// 233 against 255).
+template <int S> constexpr bool kAllLoads = S > 4;
 // Decays that a lane keeps in LDS on the way ahead for the way back.
 template <int S> constexpr int kDecays = S <= 4 ? kHeld * S : 0;
 
@@ -582,19 +595,29 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanB
     typedef typename Elem<BF16>::Type E;
     constexpr int K = kBackTile<S>;
     const Scan &s = b.s;
-    r.rows.load(s.bc, s.n, p.v, t, steps, l.lane);
-    const int64_t at = l.at(p.v, t), four = 4 * s.n * s.f;
+    const int64_t first = l.at(p.v, t), frame = s.n * s.f;
+    auto values = [&](int i, int64_t at) {
+        r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at);
+        r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at);
+        r.gy[i] = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at);
+        if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at);
+    };
+    if (kAllLoads<S>) {
+        steps = min(max(steps, 1), K);
+        r.rows.load_all(s.bc, s.n, p.v, t, steps, l.lane);
 #pragma unroll
-    for (int i = 0; i < K / 4; ++i)
-        if (4 * i + l.q < steps) {
-            r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at + i * four);
-            r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at + i * four);
-            r.gy[i] = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at + i * four);
-            if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at + i * four);
-        }
+        for (int i = 0; i < K / 4; ++i) values(i, first + (min(4 * i + l.q, steps - 1) - l.q) * frame);
 #pragma unroll
-    for (int i = 0; i < K / kHeld; ++i)
-        if (i * kHeld < steps) load_state(r.h[i], s.checkpoints + l.state(t / kHeld + i, p.v));
+        for (int i = 0; i < K / kHeld; ++i) load_state(r.h[i], s.checkpoints + l.state(t / kHeld + (i * kHeld < steps ? i : 0), p.v));
+    } else {
+        r.rows.load(s.bc, s.n, p.v, t, steps, l.lane);
+#pragma unroll
+        for (int i = 0; i < K / 4; ++i)
+            if (4 * i + l.q < steps) values(i, first + 4 * i * frame);
+#pragma unroll
+        for (int i = 0; i < K / kHeld; ++i)
+            if (i * kHeld < steps) load_state(r.h[i], s.checkpoints + l.state(t / kHeld + i, p.v));
+    }
     if (last && p.p < s.pieces - 1) load_state(r.k, s.piece_state + l.state(p.p + 1, p.v));
     else if (last && b.dh_after) load_state(r.k, b.dh_after + l.state(0, p.v));
     else if (last)
@@ -628,6 +651,10 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
     const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f, d = s.d ? s.d[l.ch] : 0.0f;
     const int at_place = J * 2 * S / 16 * place_of(lane);                 // the first value a lane has after the exchange, and where it belongs
     const int to_place = at_place / (2 * S) * 2 * N + at_place % (2 * S) / S * N + q * S + at_place % S;
+    // the thread's first value among a tile's dB and dC; values kWave further on are whole rows further on, or the same row's
+    const int row_first = threadIdx.x / (2 * N);
+    const int64_t row_at = (int64_t)row_first * s.n * 2 * N + threadIdx.x % (2 * N);
+    float *const part_out = b.dbc_part ? b.dbc_part + (int64_t)part * s.T * s.n * 2 * N : nullptr;
     auto last_tile = [&](const Place &p) { return p.t0 + (p.t1 - p.t0 - 1) / K * K; };
     Place here{slot, 0, 0, 0, 0};
     bool more = here.settle(s, s.pieces);
@@ -636,7 +663,7 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
     float x[R], dt[R], sig[R], gp[R], gz[R], h0[K / kHeld][S], k[S], from_behind[S];
     BackTile<BF16, S> r;
     auto take = [&](int steps, float *to) {
-        r.rows.stage(to, lane);
+        r.rows.template stage<kAllLoads<S>>(to, lane, steps);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             x[i] = r.x[i];
@@ -708,7 +735,7 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
                 const float dz = gz[i] * fmaf(d, x[i], quad_sums(part_y, q));
                 if (decltype(whole)::value || 4 * i + q < steps) Elem<BF16>::put(static_cast<E *>(b.dz) + at + i * four, dz);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (S > 4) __builtin_amdgcn_sched_barrier(0);                 // what the fours have in flight together does not fit the registers
         };
         auto back = [&](auto whole, int i) {          // ... and back over them
             float bc[J * 2 * S], ghb[4], sa[4];
@@ -754,7 +781,7 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
                 acc[S] = fmaf(gp[i], x[i], acc[S]);
                 acc[S + 1] += ddelta;
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (S > 4) __builtin_amdgcn_sched_barrier(0);
         };
         auto start = [&](int half) {
 #pragma unroll
@@ -801,17 +828,25 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
 #pragma unroll
             for (int i = 0; i < S + 2; ++i) { sums[i * kWave] += (double)acc[i]; acc[i] = 0.0f; }
         block_lds_sync();
-        const float *const all = s_mem + buffer * turn;
-        for (int i = threadIdx.x; i < V; i += active * kWave) {
-            const int j = i / (2 * N), column = i % (2 * N);
-            if (t + j >= here.t1) break;
-            float sum = 0.0f;
-            if (j < steps)
-                for (int o = 0; o < active; ++o) sum += all[o * V + i];
-            const int64_t to = ((int64_t)(t + j) * s.n + here.v) * 2 * N + column;
-            if (b.dbc_part) b.dbc_part[(int64_t)part * s.T * s.n * 2 * N + to] = sum;
-            else Elem<BF16>::put(static_cast<E *>(b.dbc) + to, sum);
-        }
+        // dB and dC of the tile over the workgroup's channels: reads by fours, those beyond the last wavefront of its own
+        const float *const all = s_mem + buffer * turn + threadIdx.x;
+        const int64_t tile_at = ((int64_t)t * s.n + here.v) * 2 * N + row_at;
+#pragma unroll 2
+        for (int i = 0; i < V / kWave; i += active)
+            if (i * kWave + (int)threadIdx.x < V && t + row_first + i * kWave / (2 * N) < here.t1) {
+                float sum = 0.0f;
+                for (int o = 0; o < active; o += 4) {
+                    float v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u] = all[min(o + u, active - 1) * V + i * kWave];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) sum += o + u < active ? v[u] : 0.0f;
+                }
+                if (row_first + i * kWave / (2 * N) >= steps) sum = 0.0f;
+                const int64_t to = tile_at + i * (kWave * s.n);
+                if (b.dbc_part) part_out[to] = sum;
+                else Elem<BF16>::put(static_cast<E *>(b.dbc) + to, sum);
+            }
         if (b.dh_before && here.p == 0 && t == here.t0) store_state(b.dh_before + l.state(0, here.v), k);
         buffer = ahead_buffer;
         here = next;
