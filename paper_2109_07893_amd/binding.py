@@ -831,20 +831,28 @@ def input_grad(g: torch.Tensor, w: torch.Tensor, dx: torch.Tensor, row_scale: Op
            "dgnn_input_grad")
 
 
+# The calls below are made once per timestep where a model follows a running series, on tensors that a kernel is done with in 3 us: what they
+# look at of a tensor is looked at once, and the stream is asked for as a number (0.1 us; as a Stream object 2.1).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _frames(name: str, like: torch.Tensor, *tensors: Optional[torch.Tensor]) -> None:
     """Tensors (or None) of like's shape, type and device."""
+    shape, dtype, device = like.shape, like.dtype, like.device
     for t in tensors:
-        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        if t is not None and (t.shape != shape or t.dtype is not dtype or t.device != device):
             raise ValueError(f"shape, dtype or device mismatch in {name}")
 
 
 def _floats(name: str, where: torch.Tensor, shape, *tensors: Optional[torch.Tensor]) -> None:
-    """Contiguous float32 tensors (or None) of this shape on the device of `where`."""
+    """float32 tensors (or None) of this shape on the device of `where`."""
+    device = where.device
     for t in tensors:
         if t is not None:
-            _need(t, torch.float32, name)
-            if tuple(t.shape) != tuple(shape) or t.device != where.device:
-                raise ValueError(f"{name}: expected shape {tuple(shape)} on {where.device}")
+            if t.dtype is not torch.float32:
+                _need(t, torch.float32, name)
+            if t.shape != shape or t.device != device:
+                raise ValueError(f"{name}: expected shape {tuple(shape)} on {device}")
 
 
 def _lengths(lengths: Optional[torch.Tensor], x: torch.Tensor) -> None:
@@ -856,14 +864,16 @@ def _lengths(lengths: Optional[torch.Tensor], x: torch.Tensor) -> None:
 
 def _call(x: torch.Tensor, fn, name: str, *args) -> None:
     """fn(*args, stream) on the device of x."""
-    if not x.is_cuda:
+    index = x.get_device()
+    if index < 0:
         raise ValueError(f"{name} takes tensors on the GPU")
-    if x.device.index == torch.cuda.current_device():
-        rc = fn(*args, _stream(x))
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(x.device):
-            rc = fn(*args, _stream(x))
-    _check(rc, name)
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
+    if rc != 0:
+        _check(rc, name)
 
 
 def _workspace(ws: torch.Tensor, x: torch.Tensor) -> Tuple[Optional[int], int]:

@@ -46,6 +46,19 @@ __device__ __forceinline__ int length_of(const int32_t *lengths, int64_t v, int 
 
 __device__ __forceinline__ float sigmoid_of(float a) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.44269504088896340736f)); }
 
+// N consecutive parameters from p on, N and p's place among them multiples of four: `base` needs the alignment of a float only.
+template <int N> __device__ __forceinline__ void load_parameters(float (&v)[N], const float *base, const float *p) {
+    if ((reinterpret_cast<uintptr_t>(base) & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const float4 t = *reinterpret_cast<const float4 *>(p + e);
+            v[e] = t.x; v[e + 1] = t.y; v[e + 2] = t.z; v[e + 3] = t.w;
+        }
+    } else
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = p[e];
+}
+
 // ---- forward: pieces of 16 bytes ------------------------------------------------------------------------------------
 template <bool BF16, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_kernel(Conv c) {
@@ -59,11 +72,11 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv c) {
     const int64_t frame = c.n * c.ppr;
     float taps[W][NV], bias[NV];
 #pragma unroll
-    for (int e = 0; e < NV; ++e) {
-        bias[e] = c.bias ? c.bias[(int64_t)k * NV + e] : 0.0f;
+    for (int j = 0; j < W; ++j) load_parameters<NV>(taps[j], c.taps, c.taps + (int64_t)j * c.f + k * NV);
+    if (c.bias) load_parameters<NV>(bias, c.bias, c.bias + (int64_t)k * NV);
+    else
 #pragma unroll
-        for (int j = 0; j < W; ++j) taps[j][e] = c.taps[(int64_t)j * c.f + k * NV + e];
-    }
+        for (int e = 0; e < NV; ++e) bias[e] = 0.0f;
     for (int64_t rb = blockIdx.x / c.cols; rb < c.row_blocks; rb += gridDim.x / c.cols) {
         const int64_t v = rb * c.rows_per_block + sub;
         if (v >= c.n) break;
@@ -103,14 +116,16 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv c) {
                 }
         }
         for (int t = max(t0, t_end); t < t1; ++t) y[t * frame + at] = uintx4{0, 0, 0, 0};
-        // The last W - 1 frames of the sequence.  x_after may be x_before: this lane alone has its piece, it has read what it needs of
-        // x_before (only the first piece of the time axis does), and frame j comes from a place that is not yet written.
+        // The last W - 1 frames of the sequence.  x_after may be x_before: this lane alone has its piece, and only the first piece of the time
+        // axis reads x_before.  Where that is all there is the frames are in the ring; else they are read again, frame j from a place that
+        // is not yet written.
         if (after && blockIdx.y == 0)
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
                 const int t = len - (W - 1) + j;
                 uintx4 r = {0, 0, 0, 0};
-                if (t >= 0) r = x[t * frame + at];
+                if (c.pieces == 1) r = Pack<BF16>::pack(ring[W - 2 - j]);
+                else if (t >= 0) r = x[t * frame + at];
                 else if (before) r = before[(W - 1 + t) * frame + at];
                 after[j * frame + at] = r;
             }
@@ -149,14 +164,16 @@ __global__ __launch_bounds__(kThreads) void conv_back_kernel(ConvBack b) {
     const bool mine = k < c.ppr && sub < c.rows_per_block;
     const int64_t frame = c.n * c.ppr;
     float taps[W][4], bias[4], sums[W + 1][4];
+    const int place = mine ? k : 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) load_parameters<4>(taps[j], c.taps, c.taps + (int64_t)j * c.f + place * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        bias[e] = mine && c.bias ? c.bias[(int64_t)k * 4 + e] : 0.0f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) taps[j][e] = mine ? c.taps[(int64_t)j * c.f + k * 4 + e] : 0.0f;
+        bias[e] = 0.0f;
 #pragma unroll
         for (int j = 0; j <= W; ++j) sums[j][e] = 0.0f;
     }
+    if (c.bias) load_parameters<4>(bias, c.bias, c.bias + (int64_t)place * 4);
     for (int64_t item = slot; mine && item < c.row_blocks * c.pieces; item += slots) {
         const int64_t v = item / c.pieces * c.rows_per_block + sub;
         if (v >= c.n) continue;
@@ -260,18 +277,20 @@ __global__ __launch_bounds__(kThreads) void conv_back_kernel(ConvBack b) {
     }
 }
 
-// dtaps | dbias from the workgroups' sums: sixteen strided parts of the workgroups, in 64 bits, in a fixed order.
-__global__ __launch_bounds__(256) void conv_sums_kernel(const float *__restrict__ sums, int slots, int width, int taps, float *__restrict__ dtaps, float *__restrict__ dbias,
-                                                        int accumulate) {
-    __shared__ double s_part[16][17];
+// dtaps | dbias from the workgroups' sums: 64 strided parts of them, in 64 bits, in a fixed order.
+__global__ __launch_bounds__(1024) void conv_sums_kernel(const float *__restrict__ sums, int slots, int width, int taps, float *__restrict__ dtaps, float *__restrict__ dbias,
+                                                         int accumulate) {
+    __shared__ double s_part[64][17];
     const int o = threadIdx.x % 16, r = threadIdx.x / 16, at = blockIdx.x * 16 + o;
     double sum = 0.0;
     if (at < width)
-        for (int k = r; k < slots; k += 16) sum += (double)sums[(int64_t)k * width + at];
+#pragma unroll 4
+        for (int k = r; k < slots; k += 64) sum += (double)sums[(int64_t)k * width + at];
     s_part[r][o] = sum;
     __syncthreads();
     if (r == 0 && at < width) {
-        for (int k = 1; k < 16; ++k) sum += s_part[k][o];
+#pragma unroll 7
+        for (int k = 1; k < 64; ++k) sum += s_part[k][o];
         float *to = at < taps ? dtaps + at : dbias ? dbias + (at - taps) : nullptr;
         if (to) *to = accumulate ? (float)((double)*to + sum) : (float)sum;
     }
@@ -391,7 +410,7 @@ extern "C" int dgnn_causal_conv_backward(const void *x, const float *taps, const
     }
     DGNN_RETURN_IF_LAUNCH_FAILED();
     const int width = (w + 1) * f;
-    hipLaunchKernelGGL(conv_sums_kernel, dim3((unsigned)((width + 15) / 16)), dim3(256), 0, st, b.sums, slots, width, w * f, dtaps, dbias, accumulate);
+    hipLaunchKernelGGL(conv_sums_kernel, dim3((unsigned)((width + 15) / 16)), dim3(1024), 0, st, b.sums, slots, width, w * f, dtaps, dbias, accumulate);
     DGNN_RETURN_IF_LAUNCH_FAILED();
     return DGNN_OK;
 }

@@ -3,9 +3,10 @@
 //     norm = sqrt(sum over all tensors of g^2),   out = g min(1, max_norm / (norm + 1e-6)).
 //
 // Two passes over the gradients, the second of which finds what fits the 256 MB cache there.  The tensors of a launch (their addresses
-// travel with it) are one long list of stretches of kStretch elements, shared out evenly whatever the tensors' sizes.  Squares are formed
+// travel with it) are one long list of stretches of 32 KB, shared out evenly whatever the tensors' sizes.  Squares are formed
 // and summed in 64 bits: in 32 they are infinite from 1.8e19 on and zero below 1e-23, and a multiply-add takes no longer.  A workgroup
-// of the second pass adds up the workgroups' sums by itself, in one fixed order, instead of waiting for a launch that does.
+// of the second pass adds up the workgroups' sums by itself, in one fixed order, instead of waiting for a launch that does, while its first
+// stretch is on its way.
 #include <algorithm>
 #include <vector>
 
@@ -17,7 +18,8 @@ using namespace dgnn;
 
 constexpr int kThreads = 256;
 constexpr int kTensors = 112;             // tensors of a launch
-constexpr int kStretch = 8192;            // elements of a stretch
+constexpr int kPer = 8;                   // 16-byte pieces of a stretch that a thread has
+constexpr int kPieces = kThreads * kPer;  // ... of a stretch
 constexpr int kBlocks = 1024;             // workgroups of a launch that leave a sum
 
 struct Tensors {
@@ -30,14 +32,29 @@ struct Tensors {
 };
 static_assert(sizeof(Tensors) <= 4000, "kernel arguments");
 
-// The tensor that a stretch belongs to: tensors without elements have no stretch.
-__device__ __forceinline__ int tensor_of(const Tensors &t, int64_t stretch) {
-    int lo = 0, hi = t.tensors;           // first[lo] <= stretch < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.first[mid] <= stretch) lo = mid; else hi = mid;
-    }
-    return lo;
+// Elements [from, from + count) of a tensor: `head` of them ahead of the first 16-byte boundary, `pieces` whole pieces, and what is left
+// from `tail` on (fewer than a piece each; a stretch that begins between two boundaries has both).
+struct Stretch {
+    int k, count, head, pieces, tail;
+    int64_t from;
+};
+
+// Stretch s of the list: its tensor is the last one that begins at s or ahead of it (those without elements have no stretch).  All lanes
+// look at once: a search step by step would go to the argument's memory seven times in a row.
+__device__ __forceinline__ Stretch stretch_of(const Tensors &t, int64_t s) {
+    const int lane = threadIdx.x % kWave;
+    const int below = __popcll(__ballot(lane < t.tensors && t.first[min(lane, kTensors - 1)] <= s)) +
+                      __popcll(__ballot(lane + kWave < t.tensors && t.first[min(lane + kWave, kTensors - 1)] <= s));
+    Stretch r;
+    r.k = below - 1;
+    const int size = t.bf16[r.k] ? 2 : 4, per = kPieces * (16 / size);
+    r.from = (s - t.first[r.k]) * per;
+    r.count = (int)min((int64_t)per, t.count[r.k] - r.from);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(t.g[r.k]) + r.from * size;
+    r.head = min((int)((16 - (at & 15)) & 15) / size, r.count);
+    r.pieces = (r.count - r.head) * size / 16;
+    r.tail = r.head + r.pieces * (16 / size);
+    return r;
 }
 
 // Sum over the workgroup, every thread gets it; the same order in every workgroup.
@@ -51,9 +68,6 @@ __device__ __forceinline__ double block_sum(double v, double *s_sum) {
     return v;
 }
 
-// Elements ahead of the first 16-byte boundary.
-template <typename E> __device__ __forceinline__ int ahead_of(const E *p) { return (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(E); }
-
 template <bool BF16> struct Elem;
 template <> struct Elem<false> {
     typedef float Type;
@@ -66,28 +80,31 @@ template <> struct Elem<true> {
     static __device__ __forceinline__ uint16_t put(float v) { return (uint16_t)pack_bf16(v, 0.0f); }
 };
 
-template <bool BF16> __device__ __forceinline__ double squares(const void *tensor, int64_t from, int count) {
-    typedef typename Elem<BF16>::Type E;
+template <bool BF16> __device__ __forceinline__ const typename Elem<BF16>::Type *begin_of(const Tensors &t, const Stretch &s) {
+    return as_global(static_cast<const typename Elem<BF16>::Type *>(t.g[s.k])) + s.from;
+}
+
+template <bool BF16> __device__ __forceinline__ void load(uintx4 (&r)[kPer], const Tensors &t, const Stretch &s) {
+    const uintx4 *p = reinterpret_cast<const uintx4 *>(begin_of<BF16>(t, s) + s.head) + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) r[u] = (int)threadIdx.x + u * kThreads < s.pieces ? p[u * kThreads] : uintx4{0, 0, 0, 0};
+}
+
+template <bool BF16> __device__ __forceinline__ double squares(const Tensors &t, const Stretch &s) {
     constexpr int NV = Pack<BF16>::kVals;
-    const E *g = as_global(static_cast<const E *>(tensor)) + from;
-    const int head = min(ahead_of(g), count), pieces = (count - head) / NV, tail = head + pieces * NV;
+    const auto *g = begin_of<BF16>(t, s);
+    uintx4 r[kPer];
+    load<BF16>(r, t, s);
     double sum = 0.0;
     auto one = [&](int i) { const double v = Elem<BF16>::get(g[i]); sum = fma(v, v, sum); };
-    if ((int)threadIdx.x < head) one(threadIdx.x);
-    if ((int)threadIdx.x < count - tail) one(tail + threadIdx.x);
-    const uintx4 *p = reinterpret_cast<const uintx4 *>(g + head);
-    constexpr int U = kStretch / NV / kThreads;              // all of a thread's pieces of a whole stretch
-    for (int i = threadIdx.x; i < pieces; i += kThreads * U) {
-        uintx4 r[U];
+    if ((int)threadIdx.x < s.head) one(threadIdx.x);
+    if ((int)threadIdx.x < s.count - s.tail) one(s.tail + threadIdx.x);
 #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = i + u * kThreads < pieces ? p[i + u * kThreads] : uintx4{0, 0, 0, 0};
+    for (int u = 0; u < kPer; ++u) {
+        float v[NV];
+        Pack<BF16>::unpack(v, r[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[NV];
-            Pack<BF16>::unpack(v, r[u]);
-#pragma unroll
-            for (int e = 0; e < NV; ++e) sum = fma((double)v[e], (double)v[e], sum);
-        }
+        for (int e = 0; e < NV; ++e) sum = fma((double)v[e], (double)v[e], sum);
     }
     return sum;
 }
@@ -95,11 +112,9 @@ template <bool BF16> __device__ __forceinline__ double squares(const void *tenso
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Tensors t, double *__restrict__ sums) {
     __shared__ double s_sum[kThreads / kWave];
     double sum = 0.0;
-    for (int64_t s = blockIdx.x; s < t.first[t.tensors]; s += gridDim.x) {
-        const int k = tensor_of(t, s);
-        const int64_t from = (s - t.first[k]) * kStretch;
-        const int count = (int)min((int64_t)kStretch, t.count[k] - from);
-        sum += t.bf16[k] ? squares<true>(t.g[k], from, count) : squares<false>(t.g[k], from, count);
+    for (int64_t i = blockIdx.x; i < t.first[t.tensors]; i += gridDim.x) {
+        const Stretch s = stretch_of(t, i);
+        sum += t.bf16[s.k] ? squares<true>(t, s) : squares<false>(t, s);
     }
     sum = block_sum(sum, s_sum);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -111,51 +126,52 @@ __device__ __forceinline__ double total_of(const double *__restrict__ sums, int 
     return sqrt(block_sum(sum, s_sum));
 }
 
-template <bool BF16> __device__ __forceinline__ void scaled(const void *tensor, void *to, int64_t from, int count, float factor) {
-    typedef typename Elem<BF16>::Type E;
+template <bool BF16> __device__ __forceinline__ void scaled(const uintx4 (&r)[kPer], const Tensors &t, const Stretch &s, float factor) {
     constexpr int NV = Pack<BF16>::kVals;
-    const E *g = as_global(static_cast<const E *>(tensor)) + from;
-    E *out = as_global(static_cast<E *>(to)) + from;
+    typedef typename Elem<BF16>::Type E;
+    const E *g = begin_of<BF16>(t, s);
+    E *out = as_global(static_cast<E *>(t.out[s.k])) + s.from;
     auto one = [&](int i) { out[i] = Elem<BF16>::put(Elem<BF16>::get(g[i]) * factor); };
     if ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) {       // no boundary in common
-        for (int i = threadIdx.x; i < count; i += kThreads) one(i);
+        for (int i = threadIdx.x; i < s.count; i += kThreads) one(i);
         return;
     }
-    const int head = min(ahead_of(g), count), pieces = (count - head) / NV, tail = head + pieces * NV;
-    if ((int)threadIdx.x < head) one(threadIdx.x);
-    if ((int)threadIdx.x < count - tail) one(tail + threadIdx.x);
-    const uintx4 *p = reinterpret_cast<const uintx4 *>(g + head);
-    uintx4 *o = reinterpret_cast<uintx4 *>(out + head);
-    constexpr int U = kStretch / NV / kThreads;
-    for (int i = threadIdx.x; i < pieces; i += kThreads * U) {
-        uintx4 r[U];
+    if ((int)threadIdx.x < s.head) one(threadIdx.x);
+    if ((int)threadIdx.x < s.count - s.tail) one(s.tail + threadIdx.x);
+    uintx4 *o = reinterpret_cast<uintx4 *>(out + s.head) + threadIdx.x;
 #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = i + u * kThreads < pieces ? p[i + u * kThreads] : uintx4{0, 0, 0, 0};
+    for (int u = 0; u < kPer; ++u) {
+        float v[NV];
+        Pack<BF16>::unpack(v, r[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[NV];
-            Pack<BF16>::unpack(v, r[u]);
-#pragma unroll
-            for (int e = 0; e < NV; ++e) v[e] *= factor;
-            if (i + u * kThreads < pieces) o[i + u * kThreads] = Pack<BF16>::pack(v);
-        }
+        for (int e = 0; e < NV; ++e) v[e] *= factor;
+        if ((int)threadIdx.x + u * kThreads < s.pieces) o[u * kThreads] = Pack<BF16>::pack(v);
     }
 }
 
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Tensors t, const double *__restrict__ sums, int count, double max_norm, float *__restrict__ norm) {
     __shared__ double s_sum[kThreads / kWave];
+    const int64_t stretches = t.first[t.tensors];
+    // from the end: what the first pass read last is what the cache still has
+    int64_t i = stretches - 1 - blockIdx.x;
+    Stretch s;
+    uintx4 r[kPer];
+    auto fetch = [&]() {
+        s = stretch_of(t, i);
+        if (t.bf16[s.k]) load<true>(r, t, s); else load<false>(r, t, s);
+    };
+    if (i >= 0) fetch();
     const double total = total_of(sums, count, s_sum);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
     const double most = max_norm / (total + 1e-6);
     const bool clip = isfinite(total) && most < 1.0;         // a norm that is no finite number: nothing to scale by
     const float factor = clip ? (float)most : 1.0f;
-    for (int64_t s = blockIdx.x; s < t.first[t.tensors]; s += gridDim.x) {
-        const int k = tensor_of(t, s);
-        if (!clip && t.out[k] == t.g[k]) continue;
-        const int64_t from = (s - t.first[k]) * kStretch;
-        const int n = (int)min((int64_t)kStretch, t.count[k] - from);
-        if (t.bf16[k]) scaled<true>(t.g[k], t.out[k], from, n, factor);
-        else scaled<false>(t.g[k], t.out[k], from, n, factor);
+    while (i >= 0) {
+        if (clip || t.out[s.k] != t.g[s.k]) {
+            if (t.bf16[s.k]) scaled<true>(r, t, s, factor); else scaled<false>(r, t, s, factor);
+        }
+        i -= gridDim.x;
+        if (i >= 0) fetch();
     }
 }
 
@@ -190,7 +206,8 @@ Tensors tensors_of(int32_t count, const dgnn_grad_item *items, int32_t from) {
         t.out[i] = it.out;
         t.count[i] = it.count;
         t.bf16[i] = it.dt == DGNN_BF16;
-        t.first[i + 1] = t.first[i] + (it.count + kStretch - 1) / kStretch;
+        const int64_t per = (int64_t)kPieces * (it.dt == DGNN_BF16 ? 8 : 4);
+        t.first[i + 1] = t.first[i] + (it.count + per - 1) / per;
     }
     return t;
 }
