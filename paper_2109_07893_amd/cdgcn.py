@@ -10,12 +10,13 @@ Only the LSTM ties timesteps together: snapshots are rebuilt as a series and the
 together while they are small (batch.py).  Buffers and call order only; the arithmetic is in the HIP kernels."""
 from __future__ import annotations
 
-from typing import Optional
+from typing import List, Optional
 
 import torch
 
 from . import binding as B
 from .batch import GATHERED_DINV_ROWS, Frames, SpmmTable, TransformTable, pointers, upstream_frames
+from .gradients import ClipsGradients
 from .pipeline import BlockInputs, BlockRunner
 
 # Bytes of gate gradients (N x 4 hidden per timestep) that one call of the adjoint leaves for the weight gradients behind it.
@@ -186,7 +187,7 @@ class CdgcnLayer(BlockRunner):
         return self.h_all
 
 
-class CdgcnTrainer(CdgcnLayer):
+class CdgcnTrainer(ClipsGradients, CdgcnLayer):
     """Forward and backward over one block for the CD-GCN layer (Section "CD-GCN", trained as in Section "Gradient
     Checkpoint": the forward pass keeps only the LSTM states (h_t, c_t) of every timestep, and Y0 and Y where they are asked
     for; the backward pass walks the timesteps in reverse, recomputing what was not kept):
@@ -319,6 +320,9 @@ class CdgcnTrainer(CdgcnLayer):
             self._backward_stretches(g_h)
         else:
             self._backward_steps(g_h)
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return [self.dw, self.dw_x, self.dw_h, self.db]
 
     def _backward_stretches(self, g_h: torch.Tensor) -> None:
         blk, steps = self.blk, self.back_steps

@@ -14,9 +14,10 @@ from typing import List
 import torch
 
 from . import binding as B
+from .gradients import ClipsGradients
 
 
-class EvolvingWeights:
+class EvolvingWeights(ClipsGradients):
     def __init__(self, w0: torch.Tensor, u_x: torch.Tensor, u_h: torch.Tensor, bias: torch.Tensor, T: int):
         f, f2 = w0.shape
         assert w0.dtype == torch.float32 and tuple(u_x.shape) == (f2, 4 * f2) and tuple(u_h.shape) == (f2, 4 * f2)
@@ -39,3 +40,6 @@ class EvolvingWeights:
     def backward(self, dw_t: List[torch.Tensor]) -> None:
         """dw_t[t-1] = dL/dW_t (fp32, from the GCN steps).  Leaves dL/dU_x, dL/dU_h, dL/db and dL/dW_0."""
         B.evolve_weights_backward(self.w0, self.u_x, self.u_h, self.bias, self.w, self.c, dw_t, self.dw0, self.du_x, self.du_h, self.db, self.ws)
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return [self.dw0, self.du_x, self.du_h, self.db]

@@ -2,7 +2,7 @@
 (Section "Gradient Checkpoint") and the update of the weights.  A table of the tensors and a workspace; the arithmetic is in the HIP kernels."""
 from __future__ import annotations
 
-from typing import Optional, Sequence
+from typing import List, Optional, Sequence
 
 import torch
 
@@ -28,13 +28,17 @@ class Gradients:
             if o.shape != g.shape or o.dtype != g.dtype or g.device != dev or o.device != dev:
                 raise ValueError("shape, dtype or device mismatch in Gradients")
         self.table = Table(len(self.grads), 4)
-        self.table.column(self.G, [B._ptr(g) or 0 for g in self.grads])
-        self.table.column(self.OUT, [B._ptr(o) or 0 for o in self.out])
+        self.bind()
         self.table.column(self.COUNT, [g.numel() for g in self.grads])
         self.table.column(self.DT, [B._dtype_code(g) for g in self.grads])
         self.result = torch.zeros(1, dtype=torch.float32, device=dev)
         self.scalar = self.result[0]
         self.ws = torch.empty(B.grad_clip_workspace(len(self.grads)), dtype=torch.uint8, device=dev)
+
+    def bind(self) -> None:
+        """The addresses as they are now (after a tensor was given other memory, which is rare)."""
+        self.table.column(self.G, [B._ptr(g) or 0 for g in self.grads])
+        self.table.column(self.OUT, [B._ptr(o) or 0 for o in self.out])
 
     def norm(self) -> torch.Tensor:
         """sqrt(sum g^2) over all of them: a scalar on the device, overwritten by the next call."""
@@ -45,3 +49,24 @@ class Gradients:
         """out = g min(1, max_norm / (norm + 1e-6)); returns the norm from before.  A norm that is no finite number changes nothing."""
         B.grad_clip(len(self.grads), self.table.at(), max_norm, self.result, self.ws)
         return self.scalar
+
+
+class ClipsGradients:
+    """What a trainer has to do with its gradients before they are applied: clip_gradients() between backward() and the update."""
+
+    _clipped = None
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        """The gradients that backward() leaves."""
+        raise NotImplementedError
+
+    def clip_gradients(self, max_norm: float) -> torch.Tensor:
+        """Scales them, where they lie, so that the norm over all of them is at most max_norm; returns the norm from before, a scalar on
+        the device.  A norm that is no finite number changes nothing."""
+        grads = self.parameter_gradients()
+        bound = self._clipped
+        if bound is None or len(bound.grads) != len(grads) or any(a is not b for a, b in zip(bound.grads, grads)):
+            bound = self._clipped = Gradients(grads)
+        else:
+            bound.bind()
+        return bound.clip(max_norm)

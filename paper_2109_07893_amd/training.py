@@ -33,6 +33,7 @@ import torch
 
 from . import binding as B
 from .batch import GATHERED_DINV_ROWS, SERIES_ENTRIES, Frames, SeriesTable, SmoothTable, SpmmTable, TransformTable, WeightGradTable, pointers, series_pays, snapshots_fit, steps_together, upstream_frames
+from .gradients import ClipsGradients
 from .pipeline import BlockInputs, BlockRunner
 
 
@@ -255,7 +256,7 @@ class GcnStack:
             g = dst
 
 
-class BlockTrainer:
+class BlockTrainer(ClipsGradients):
     """Forward and backward over one block; gradients of the layer weights (fp32) come out in `dw`."""
 
     def __init__(self, blk: BlockInputs, directed: bool,
@@ -417,6 +418,9 @@ class BlockTrainer:
                     self._rebuild(chain, lists[t - 1], blk.nnz[t], t + 1, t, reverse=True)
 
 
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return self.dw if self.dw_t is None else [g for t in range(self.blk.T) for g in self.dw_t[t]]
+
     @property
     def h(self) -> torch.Tensor:
         """The first layer's G_H = A~_1^T G_P of the block's first timestep, the last one that backward() takes.  Where the step
@@ -500,7 +504,7 @@ def make_trainer(wl, blk: BlockInputs, want_dx: bool = False, keep_snapshots: bo
                         keep_snapshots=keep_snapshots)
 
 
-class CheckpointedTrainer:
+class CheckpointedTrainer(ClipsGradients):
     """The paper's gradient checkpointing over a series of T timesteps cut into blocks (Section "Gradient
     Checkpoint"): a forward pass block by block that keeps only what the next block needs (the last w - 1 frames
     of Z; here also each block's first snapshot, which the paper sends whole), then, from the last block to the
@@ -547,6 +551,11 @@ class CheckpointedTrainer:
         a, e = self.bounds[b]
         t_first = None if self.t_first is None else (self.t_first[b][0], self.t_first[b][1][: self.series.nnz[a]])
         self.trainer.rebind(self._block(b), t0=a, z_before=self.pi[b], transposed_first=t_first, transposed_deltas=self._t_deltas(a, e))
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        if self.series.w_t is not None:
+            raise ValueError("one weight per timestep: the gradients of a block make room for the next one's")
+        return self.dw
 
     def forward(self, on_block=None) -> None:
         """Block by block; on_block(b, a, e, y) sees the block's output frames before they are overwritten."""
@@ -609,7 +618,7 @@ class _Ring:
         return self.rowptr[s], self.colidx[s], nnz
 
 
-class SmoothedTrainer:
+class SmoothedTrainer(ClipsGradients):
     """A training step on SMOOTHED snapshots (Section "Smoothening the Input Graphs": the graphs TM-GCN and EvolveGCN
     are trained on), with the smoothing done on the device: every S_t and its normalisation by dgnn_smooth_series, or, for
     series longer than one such call takes, the raw A_t by dgnn_delta_rebuild, S_t = S_{t-1} + A_t - A_{t-life} by
@@ -724,6 +733,9 @@ class SmoothedTrainer:
             rp, _, val = self.s[t - 1]
             with self._stage("csr_weighted_dinv"):
                 B.csr_weighted_dinv(rp, val, self.s_nnz[t - 1], self.dinv_s[t - 1], self.ws_dinv)
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return self.dw if self.dw_t is None else [g for t in range(self.blk.T) for g in self.dw_t[t]]
 
     def forward(self) -> torch.Tensor:
         blk, stack = self.blk, self.stack

@@ -1,0 +1,233 @@
+"""The state-space layer as a whole, and the operators in a run as they are used: GCN frames below it, gradients back through both, clipped.
+
+The layer is checked against the same composition in 64 bits (the oracle's operators and plain products); fp32 results pass through five
+products and two operators one after the other, whose errors add up to some 2^-20 of the magnitudes that meet (each is tested on its own
+to 2^-24 times its depth): 2e-5 of the result's norm and 2e-4 of its largest entries leave room for magnitudes ten times the result."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2109_07893_amd as dg
+from dtdg_synth import WORKLOADS
+from dtdg_synth.blocks import make_block
+from oracle import temporal as tp
+from paper_2109_07893_amd.cdgcn import CdgcnTrainer
+from paper_2109_07893_amd.evolve import EvolvingWeights
+from paper_2109_07893_amd.statespace import PARAMETERS, WEIGHTS, StateSpaceLayer
+from paper_2109_07893_amd.training import CheckpointedTrainer, make_smoothed_trainer, make_trainer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def np64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def make_weights(f, d, states, w, dtype=torch.float32, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    s = lambda *shape: torch.randn(shape, generator=g)  # noqa: E731
+    p = dict(w_in=s(f, d) * f ** -0.5, w_z=s(f, d) * f ** -0.5, w_dt=0.3 * s(d, d) * d ** -0.5, w_bc=s(d, 2 * states) * d ** -0.5, w_out=s(d, f) * d ** -0.5)
+    p = {k: v.to(dtype) for k, v in p.items()}
+    p.update(taps=0.5 * s(w, d), conv_bias=0.1 * s(d), a=-torch.arange(1, states + 1).float() * torch.exp(0.2 * s(d, states)), d=1 + 0.1 * s(d), dt_bias=s(d) - 3)
+    return {k: v.to(DEV).contiguous() for k, v in p.items()}
+
+
+def oracle_layer(p, x, g_out, lengths, frames=None, state=None):
+    q = {k: np64(v) for k, v in p.items()}
+    x, g_out = np64(x), np64(g_out)
+    u0, z = x @ q["w_in"], x @ q["w_z"]
+    conv = dict(taps=q["taps"], bias=q["conv_bias"], act=True, x_before=frames, lengths=lengths)
+    u, _ = tp.causal_conv(u0, **conv)
+    scan = dict(x=u, delta=u @ q["w_dt"], bc=u @ q["w_bc"], a=q["a"], z=z, d=q["d"], dt_bias=q["dt_bias"], h_before=state, lengths=lengths)
+    y, _, _ = tp.selective_scan(**scan)
+    g = tp.selective_scan_backward(g_y=g_out @ q["w_out"].T, **scan)
+    du = g["dx"] + g["ddelta"] @ q["w_dt"].T + g["dbc"] @ q["w_bc"].T
+    c = tp.causal_conv_backward(u0, g_y=du, **conv)
+    rows = lambda a, b: a.reshape(-1, a.shape[-1]).T @ b.reshape(-1, b.shape[-1])  # noqa: E731
+    grads = dict(w_out=rows(y, g_out), w_dt=rows(u, g["ddelta"]), w_bc=rows(u, g["dbc"]), w_in=rows(x, c["dx"]), w_z=rows(x, g["dz"]), taps=c["dtaps"],
+                 conv_bias=c["dbias"], a=g["da"], d=g["dd"], dt_bias=g["ddt_bias"])
+    return y @ q["w_out"], c["dx"] @ q["w_in"].T + g["dz"] @ q["w_z"].T, grads
+
+
+def near(got, want, what, norm=2e-5, worst=2e-4):
+    got = np64(got)
+    assert np.isfinite(got).all(), what
+    assert np.linalg.norm(got - want) <= norm * np.linalg.norm(want) + 1e-30, (what, np.linalg.norm(got - want) / np.linalg.norm(want))
+    assert np.abs(got - want).max() <= worst * np.abs(want).max() + 1e-30, what
+
+
+@pytest.mark.parametrize("T,n,f,d,states,w,ragged", [(1, 33, 16, 32, 8, 4, False), (21, 10, 32, 64, 16, 4, False), (40, 7, 64, 128, 32, 3, True), (5, 300, 16, 16, 8, 2, True)])
+def test_layer(T, n, f, d, states, w, ragged):
+    p = make_weights(f, d, states, w)
+    g = torch.Generator().manual_seed(5)
+    lengths = torch.randint(0, T + 1, (n,), generator=g, dtype=torch.int32) if ragged else None
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV), torch.randn((T, n, f), generator=g).to(DEV)
+    layer = StateSpaceLayer(n, T, p, lengths=None if lengths is None else lengths.to(DEV))
+    out = layer.forward(x, train=True).clone()
+    dx = layer.backward(g_out)
+    want, want_dx, grads = oracle_layer(p, x, g_out, None if lengths is None else lengths.numpy())
+    near(out, want, "out")
+    near(dx, want_dx, "dx")
+    for k in WEIGHTS + PARAMETERS:
+        near(layer.grads[k], grads[k], k)
+
+
+def test_steps_follow_the_series():
+    """The series at once, and one timestep at a time from the state that a first block leaves."""
+    T, n, f, cut = 12, 50, 32, 5
+    p = make_weights(f, 64, 16, 4)
+    x = torch.randn((T, n, f), generator=torch.Generator().manual_seed(1)).to(DEV)
+    whole = StateSpaceLayer(n, T, p).forward(x)
+    layer = StateSpaceLayer(n, cut, p)
+    parts = [layer.forward(x[:cut].contiguous()).clone()] + [layer.step(x[t]).clone()[None] for t in range(cut, T)]
+    assert torch.equal(torch.cat(parts), whole)
+    layer.reset()
+    assert torch.equal(layer.forward(x[:cut].contiguous()), whole[:cut])
+
+
+def test_blocks_hand_over():
+    """Two blocks, the state handed over and its gradients back, against the series in one."""
+    T, n, f = 14, 20, 16
+    p = make_weights(f, 32, 8, 4)
+    g = torch.Generator().manual_seed(2)
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV), torch.randn((T, n, f), generator=g).to(DEV)
+    want, want_dx, grads = oracle_layer(p, x, g_out, None)
+    first, second = StateSpaceLayer(n, 9, p), StateSpaceLayer(n, 5, p)
+    out = [first.forward(x[:9].contiguous(), train=True)]
+    second.frames.copy_(first.frames)
+    second.state.copy_(first.state)
+    out.append(second.forward(x[9:].contiguous(), train=True))
+    dx = [second.backward(g_out[9:].contiguous())]
+    dx.insert(0, first.backward(g_out[:9].contiguous(), behind=(second.dframes, second.dstate)))
+    near(torch.cat(out), want, "out")
+    near(torch.cat(dx), want_dx, "dx")
+    for k in WEIGHTS + PARAMETERS:
+        near(first.grads[k] + second.grads[k], grads[k], k)
+
+
+def test_bf16_layer_runs():
+    """bf16 frames: every tensor between the steps is rounded to 2^-9; results within a few per cent of the same weights in 64 bits."""
+    T, n, f = 18, 64, 32
+    p = make_weights(f, 64, 16, 4, dtype=torch.bfloat16)
+    g = torch.Generator().manual_seed(3)
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV).bfloat16(), torch.randn((T, n, f), generator=g).to(DEV).bfloat16()
+    layer = StateSpaceLayer(n, T, p)
+    out = layer.forward(x, train=True).clone()
+    dx = layer.backward(g_out)
+    want, want_dx, grads = oracle_layer(p, x, g_out, None)
+    near(out, want, "out", 0.03, 0.1)
+    near(dx, want_dx, "dx", 0.05, 0.2)
+    for k in WEIGHTS:
+        near(layer.grads[k], grads[k], k, 0.05, 0.2)
+
+
+def total(grads):
+    return float(np.sqrt(sum(float((g.double() ** 2).sum()) for g in grads)))
+
+
+def check_clip(trainer, max_norm):
+    grads = trainer.parameter_gradients()
+    before, norm = [g.clone() for g in grads], total(grads)
+    assert norm > max_norm
+    assert float(trainer.clip_gradients(max_norm)) == pytest.approx(norm, rel=2e-7)
+    for a, b in zip(before, grads):
+        assert torch.allclose(b.double(), a.double() * (max_norm / (norm + 1e-6)), rtol=2.0 ** -22, atol=0)
+    assert float(trainer.clip_gradients(max_norm)) <= max_norm * (1 + 1e-6)
+
+
+def test_training_run():
+    """A GCN block, the layer over its frames, gradients back through both, clipped together: three steps."""
+    wl = WORKLOADS["c1"]
+    blk = make_block(wl, DEV, gen_device="cpu")
+    gcn = make_trainer(wl, blk)
+    layer = StateSpaceLayer(wl.n, wl.T, make_weights(wl.f, 32, 8, 4))
+    target = torch.randn((wl.T, wl.n, wl.f), generator=torch.Generator().manual_seed(9)).to(DEV)
+    clipper = None
+    for _ in range(3):
+        layer.reset()
+        out = layer.forward(gcn.forward(), train=True)
+        dx = layer.backward(out - target)
+        gcn.backward(dx)
+        grads = gcn.parameter_gradients() + layer.parameter_gradients()
+        norm = total(grads)
+        clipper = clipper or dg.Gradients(grads)
+        assert float(clipper.clip(0.5)) == pytest.approx(norm, rel=1e-6)
+        assert all(torch.isfinite(g).all() for g in grads) and total(grads) <= 0.5 * (1 + 1e-6)
+        for w, g in zip([blk.w[0]] + [layer.weights[k] for k in layer.grads], grads):
+            w -= 0.1 * g.to(w.dtype)
+
+
+def test_layer_in_a_graph():
+    """Forward, backward and clipping recorded; every replay against the eager result, with eager work between."""
+    T, n, f = 10, 30, 16
+    p = make_weights(f, 32, 8, 4)
+    g = torch.Generator().manual_seed(4)
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV), torch.randn((T, n, f), generator=g).to(DEV)
+    layer = StateSpaceLayer(n, T, p)
+
+    def work():
+        layer.reset()
+        layer.forward(x, train=True)
+        layer.backward(g_out)
+        return layer.clip_gradients(1.0)
+
+    norm = work().clone()
+    eager = [t.clone() for t in [layer.out, layer.dx] + layer.parameter_gradients()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for _ in range(3):
+        for t in [layer.out, layer.dx] + layer.parameter_gradients():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layer._clipped.scalar, norm)
+        assert all(torch.equal(a, b) for a, b in zip(eager, [layer.out, layer.dx] + layer.parameter_gradients()))
+        StateSpaceLayer(n, T, p).forward(x)
+
+
+def test_trainers_clip():
+    wl = WORKLOADS["c1"]
+    blk = make_block(wl, DEV, gen_device="cpu")
+    g_y = torch.randn((wl.T, wl.n, wl.f), generator=torch.Generator().manual_seed(1)).to(DEV)
+    tr = make_trainer(wl, blk)
+    tr.forward()
+    tr.backward(g_y)
+    check_clip(tr, 0.01)
+    tr = make_smoothed_trainer(wl, blk, 3)
+    tr.forward()
+    tr.backward(g_y)
+    check_clip(tr, 0.01)
+    tr = CheckpointedTrainer(wl, blk, 4)
+    tr.forward()
+    tr.backward(g_y)
+    check_clip(tr, 0.01)
+    f = wl.f
+    r = lambda *s: 0.3 * torch.randn(s, generator=torch.Generator().manual_seed(len(s))).to(DEV)  # noqa: E731
+    ev = EvolvingWeights(r(f, f), r(f, 4 * f), r(f, 4 * f), r(4 * f).view(-1), wl.T)
+    blk.w_t = [[w] for w in ev.forward()]
+    tr = make_trainer(wl, blk)
+    tr.forward()
+    tr.backward(g_y)
+    ev.backward([g[0] for g in tr.dw_t])
+    check_clip(ev, 0.01)
+    check_clip(tr, 0.01)
+    blk.w_t = None
+    tr = CdgcnTrainer(blk, r(f, f), r(2 * f, 4 * f), r(f, 4 * f), r(4 * f).view(-1), f)
+    tr.forward()
+    tr.backward(g_y)
+    check_clip(tr, 0.01)
+
+
+def test_refusals():
+    p = make_weights(16, 32, 8, 4)
+    with pytest.raises(ValueError):
+        StateSpaceLayer(4, 3, dict(p, a=p["a"][:, :4]))
+    with pytest.raises(ValueError):
+        StateSpaceLayer(4, 3, dict(p, taps=p["taps"].bfloat16()))
+    layer = StateSpaceLayer(4, 3, p)
+    with pytest.raises(ValueError):
+        layer.forward(torch.zeros((2, 4, 16), device=DEV))
+    with pytest.raises(ValueError):
+        layer.step(torch.zeros((4, 16), device=DEV, dtype=torch.bfloat16))
