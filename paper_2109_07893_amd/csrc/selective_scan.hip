@@ -32,9 +32,11 @@ constexpr int kChannels = 16;             // channels of a wavefront
 constexpr int kTile = 16;                 // timesteps of a tile
 constexpr int kHeld = 8;                  // ... between two kept states: the adjoint holds the states of so many in registers
 constexpr int kWaves = 4;                 // wavefronts of a workgroup of the kernels without sums over channels
-constexpr int kBackWaves = 8;             // ... of the adjoint, at most
+// Wavefronts of a workgroup of the adjoint at most, and of all its workgroups: two on a SIMD, and three with 8 states, whose registers
+// allow it (2^17 x 128 fp32: 226 us with two, 193 with three); workgroups of four then, for three times eight do not fit.
+constexpr int back_waves(int states) { return states == 8 ? 4 : 8; }
+constexpr int back_resident(int states) { return states == 8 ? 3072 : 2048; }
 constexpr int kMaxGrid = 1 << 22;         // workgroups of a launch: HIP counts its threads in 32 bits
-constexpr int kBackResident = 2048;       // ... of all its workgroups: two on a SIMD
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;
 constexpr float kLn2 = 0.693147180559945309417f;
@@ -274,15 +276,22 @@ template <bool BF16, int S> struct Tile {
 template <bool BF16, int S, bool Y, bool GATE>
 __device__ __forceinline__ void load_tile(Tile<BF16, S> &r, const Scan &s, const Lane<S> &l, int64_t v, int t, int steps, bool first) {
     typedef typename Elem<BF16>::Type E;
-    r.rows.load(s.bc, s.n, v, t, steps, l.lane);
-    const int64_t at = l.at(v, t), four = 4 * s.n * s.f;
+    const int64_t first_at = l.at(v, t), four = 4 * s.n * s.f;
+    auto values = [&](int i) {
+        r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + first_at + i * four);
+        r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + first_at + i * four);
+        if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + first_at + i * four);
+    };
+    if (S <= 4 && steps == kTile) {       // no lane stands aside: nothing for the compiler to wait for ahead of the loads (4 - 7 %; with 32 states it costs that)
+        r.rows.load_all(s.bc, s.n, v, t, kTile, l.lane);
 #pragma unroll
-    for (int i = 0; i < kTile / 4; ++i)
-        if (4 * i + l.q < steps) {
-            r.x[i] = Elem<BF16>::get(static_cast<const E *>(s.x) + at + i * four);
-            r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + at + i * four);
-            if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at + i * four);
-        }
+        for (int i = 0; i < kTile / 4; ++i) values(i);
+    } else {
+        r.rows.load(s.bc, s.n, v, t, steps, l.lane);
+#pragma unroll
+        for (int i = 0; i < kTile / 4; ++i)
+            if (4 * i + l.q < steps) values(i);
+    }
     if (first && s.h_before && (Y ? s.pieces == 1 : t == 0)) load_state(r.h, s.h_before + l.state(0, v));
     else if (first)
 #pragma unroll
@@ -474,30 +483,47 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
 
 // The states between the pieces, in place.  Forward (STEP 1): piece p left part[p] behind when it started from zero, part[0] from h_before;
 // the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
-// reaches piece p from behind takes the place p + 1.  A lane has one state and fetches kJoin pieces' parts together.
-constexpr int kJoin = 32;
-template <int STEP> __global__ __launch_bounds__(256) void join_kernel(Scan s, const float *behind, int states) {
-    const int64_t width = s.n * s.f * states, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= width) return;
-    const int64_t c = i / states;
+// reaches piece p from behind takes the place p + 1.  A thread has one state of one of RUNS runs of pieces, kJoin of them fetched together:
+// what a run does to a state (its own part, its decay) first, then the runs ahead of it one after the other, then its pieces.  Runs are for
+// many pieces of few states (147 of 6144: 7.7 us with sixteen runs, 15 with one; 10 of 98304, which then lie in lines of their own: 24 and 5).
+constexpr int kJoin = 16, kJoinThreads = 256;
+template <int STEP, int RUNS> __global__ __launch_bounds__(kJoinThreads) void join_kernel(Scan s, const float *behind, int states) {
+    constexpr int STATES = kJoinThreads / RUNS;
+    __shared__ float s_part[RUNS][STATES], s_time[RUNS][STATES];
+    const int64_t width = s.n * s.f * states;                                // a multiple of sixteen; beyond it: its last state once more
+    const int o = threadIdx.x % STATES, run = threadIdx.x / STATES;
+    const int64_t at = (int64_t)blockIdx.x * STATES + o, i = min(at, width - 1), c = i / states;
     const float a2 = s.a[c % s.f * states + i % states] * kLog2e;
-    const int first = STEP > 0 ? 1 : s.pieces - 1, count = s.pieces - (STEP > 0 ? 2 : 1);
-    float h = STEP > 0 ? s.piece_state[i] : behind ? behind[i] : 0.0f;
-    for (int k = 0; k < count; k += kJoin) {
-        float part[kJoin], time[kJoin];
+    const int first = STEP > 0 ? 1 : s.pieces - 1, count = s.pieces - (STEP > 0 ? 2 : 1), per = (count + RUNS - 1) / RUNS;
+    const int k0 = run * per, k1 = min(count, k0 + per);
+    auto pieces = [&](float h, float &time, bool store) {
+        time = 0.0f;
+        for (int k = k0; k < k1; k += kJoin) {
+            float part[kJoin], step[kJoin];
 #pragma unroll
-        for (int j = 0; j < kJoin; ++j) {
-            const int p = first + STEP * min(k + j, count - 1);
-            part[j] = s.piece_state[p * width + i];
-            time[j] = s.piece_time[p * s.n * s.f + c];
-        }
-#pragma unroll
-        for (int j = 0; j < kJoin; ++j)
-            if (k + j < count) {
-                h = fmaf(exp2_of(time[j] * a2), h, part[j]);
-                s.piece_state[(first + STEP * (k + j)) * width + i] = h;
+            for (int j = 0; j < kJoin; ++j) {
+                const int p = first + STEP * min(k + j, k1 - 1);
+                part[j] = s.piece_state[p * width + i];
+                step[j] = s.piece_time[p * s.n * s.f + c];
             }
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j)
+                if (k + j < k1) {
+                    h = fmaf(exp2_of(step[j] * a2), h, part[j]);
+                    time += step[j];
+                    if (store && at < width) s.piece_state[(first + STEP * (k + j)) * width + i] = h;
+                }
+        }
+        return h;
+    };
+    float time, h = STEP > 0 ? s.piece_state[i] : behind ? behind[i] : 0.0f;
+    if (RUNS > 1) {
+        s_part[run][o] = pieces(0.0f, time, false);
+        s_time[run][o] = time;
+        __syncthreads();
+        for (int r = 0; r < run; ++r) h = fmaf(exp2_of(s_time[r][o] * a2), h, s_part[r][o]);
     }
+    pieces(h, time, true);
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
@@ -575,7 +601,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
 }
 
 // Timesteps of a tile of the adjoint: what a wavefront fetches ahead.
-template <int S> constexpr int kBackTile = S <= 4 ? 16 : 8;
+template <int S> constexpr int kBackTile = S == 4 ? 16 : 8;
 // Whether a tile's loads are all made, whatever is there of it.  With 32 states, where the registers are short, the loads that a branch may
 // pass over cost more (2^17 x 128 fp32: 922 us against 658); with 16 and 8 the addresses that take the branches' place do (338 against 382,
 // 233 against 255).
@@ -625,9 +651,9 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanB
         for (int i = 0; i < S; ++i) r.k[i] = 0.0f;
 }
 
-// A workgroup has all channels of a sequence, or a part of them (of kBackWaves wavefronts).
+// A workgroup has all channels of a sequence, or a part of them (of back_waves() wavefronts).
 template <bool BF16, int S, bool GATE>
-__global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b) {
+__global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
     constexpr int N = 4 * S, K = kBackTile<S>, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
     constexpr int J = S <= 4 ? 4 : 2;                                     // timesteps whose sums over channels are exchanged together
@@ -638,7 +664,7 @@ __global__ __launch_bounds__(kBackWaves *kWave) void scan_back_kernel(ScanBack b
     const Scan &s = b.s;
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int part = blockIdx.x % b.blocks_of_groups, slot = blockIdx.x / b.blocks_of_groups, slots = gridDim.x / b.blocks_of_groups;
-    const int g = part * kBackWaves + wave, active = min(waves, s.groups - part * kBackWaves);
+    const int g = part * back_waves(N) + wave, active = min(waves, s.groups - part * back_waves(N));
     if (wave >= active) return;                                           // the last part may be narrower; a barrier waits for those that are left
     const Lane<S> l(s, g, lane);
     const int q = l.q, turn = waves * V;
@@ -917,12 +943,12 @@ Pieces forward_pieces(int64_t T, int64_t n, int32_t f) { return pieces_of(T, n *
 
 struct BackShape { int groups, blocks_of_groups, waves; Pieces pieces; int64_t slots; };
 
-BackShape back_shape(int64_t T, int64_t n, int32_t f) {
+BackShape back_shape(int64_t T, int64_t n, int32_t f, int32_t N) {
     BackShape b;
     b.groups = f / kChannels;
-    b.blocks_of_groups = (b.groups + kBackWaves - 1) / kBackWaves;
-    b.waves = std::min(b.groups, kBackWaves);
-    const int64_t blocks = std::max(1, kBackResident / (b.waves * b.blocks_of_groups));
+    b.blocks_of_groups = (b.groups + back_waves(N) - 1) / back_waves(N);
+    b.waves = std::min(b.groups, back_waves(N));
+    const int64_t blocks = std::max(1, back_resident(N) / (b.waves * b.blocks_of_groups));
     b.pieces = pieces_of(T, n, blocks);
     b.slots = std::min<int64_t>(n * b.pieces.count, blocks);
     return b;
@@ -955,6 +981,14 @@ template <typename F> int by_kind(dgnn_dtype dt, int32_t N, F &&launch) {
     if (N == 8) { if (wide) launch(std::integral_constant<bool, true>{}, std::integral_constant<int, 2>{}); else launch(std::integral_constant<bool, false>{}, std::integral_constant<int, 2>{}); }
     else if (N == 16) { if (wide) launch(std::integral_constant<bool, true>{}, std::integral_constant<int, 4>{}); else launch(std::integral_constant<bool, false>{}, std::integral_constant<int, 4>{}); }
     else { if (wide) launch(std::integral_constant<bool, true>{}, std::integral_constant<int, 8>{}); else launch(std::integral_constant<bool, false>{}, std::integral_constant<int, 8>{}); }
+    DGNN_RETURN_IF_LAUNCH_FAILED();
+    return DGNN_OK;
+}
+
+template <int STEP> int join_pieces(const Scan &s, const float *behind, int32_t states, hipStream_t st) {
+    const int64_t width = s.n * s.f * states;
+    if (s.pieces > 2 * kJoin) hipLaunchKernelGGL((join_kernel<STEP, 16>), dim3((unsigned)(width / 16)), dim3(kJoinThreads), 0, st, s, behind, states);
+    else hipLaunchKernelGGL((join_kernel<STEP, 1>), dim3((unsigned)((width + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st, s, behind, states);
     DGNN_RETURN_IF_LAUNCH_FAILED();
     return DGNN_OK;
 }
@@ -1010,8 +1044,7 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
         });
         if (rc) return rc;
         if (s.pieces > 2) {
-            hipLaunchKernelGGL(join_kernel<1>, dim3((unsigned)((n * f * states + 255) / 256)), dim3(256), 0, st, s, (const float *)nullptr, states);
-            DGNN_RETURN_IF_LAUNCH_FAILED();
+            if (const int failed = join_pieces<1>(s, nullptr, states, st)) return failed;
         }
     }
     if (T == 1)
@@ -1028,7 +1061,7 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
 extern "C" int dgnn_selective_scan_backward_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes) {
     if (!bytes) return DGNN_ERR_NULL;
     if (int rc = check_shape(T, n, f, states)) return rc;
-    const BackShape b = back_shape(T, n, f);
+    const BackShape b = back_shape(T, n, f, states);
     *bytes = piece_bytes(b.pieces, n, f, states) + round_up((size_t)b.slots * f * (states + 2) * sizeof(double), 256) +
              (b.blocks_of_groups > 1 ? (size_t)b.blocks_of_groups * T * n * 2 * states * sizeof(float) : 0);
     return DGNN_OK;
@@ -1059,7 +1092,7 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
         for (size_t k = 0; k < i; ++k)
             if (overlap(out[i].first, out[i].second, out[k].first, out[k].second)) return DGNN_ERR_ALIAS;
     }
-    const BackShape shape = back_shape(T, n, f);
+    const BackShape shape = back_shape(T, n, f, states);
     ScanBack b{};
     b.s = Scan{x, delta, bc, z, a, d, dt_bias, nullptr, nullptr, nullptr, const_cast<float *>(checkpoints), lengths, n, (int)T, f, shape.groups, 0, 0, nullptr, nullptr};
     place_pieces(b.s, shape.pieces, states, ws);
@@ -1076,8 +1109,7 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
             hipLaunchKernelGGL(kernel, walk_grid(kernel, b.s, b.s.pieces - 1), dim3(kWaves * kWave), 0, st, b);
         });
         if (rc) return rc;
-        hipLaunchKernelGGL(join_kernel<-1>, dim3((unsigned)((n * f * states + 255) / 256)), dim3(256), 0, st, b.s, dh_after, states);
-        DGNN_RETURN_IF_LAUNCH_FAILED();
+        if (const int failed = join_pieces<-1>(b.s, dh_after, states, st)) return failed;
     }
     int rc = by_kind(dt, states, [&](auto bf16, auto per) {
         constexpr int S = decltype(per)::value;
