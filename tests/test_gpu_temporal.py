@@ -222,7 +222,7 @@ def test_scan(T, n, f, N, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("T,n,f,N", [(20, 2, 144, 16), (18, 3, 400, 8), (9, 1, 2064, 32), (6, 700, 16, 16), (2, 1500, 128, 16)])
+@pytest.mark.parametrize("T,n,f,N", [(20, 2, 144, 16), (18, 3, 400, 8), (9, 1, 2064, 32), (6, 700, 16, 16), (2, 1500, 128, 16), (2, 1, 16384, 8), (17, 1, 15984, 8)])
 def test_scan_wide_and_many(T, n, f, N, dtype):
     Scan(T, n, f, N, dtype, seed=f).check()
 
@@ -233,6 +233,12 @@ def test_scan_wide_and_many(T, n, f, N, dtype):
 def test_scan_in_pieces(T, n, f, N, dtype):
     """Few sequences, many timesteps: the time axis is shared out."""
     Scan(T, n, f, N, dtype, seed=T).check()
+
+
+@pytest.mark.parametrize("N", [8, 32])
+def test_scan_very_long(N):
+    """Thousands of pieces, joined in runs of many."""
+    Scan(70_001, 1, 16, N, F32, seed=N).check()
 
 
 @pytest.mark.parametrize("N", [8, 16, 32])
@@ -350,11 +356,22 @@ def test_offsets_beyond_32_bits():
     dg.selective_scan(x, delta, bc, a, y, ws, h_after=h)
     dg.selective_scan(*cut, a, y1, ws, h_after=h1)
     assert torch.equal(y[:, -tail:], y1) and torch.equal(h[-tail:], h1)
+    back = []
+    for q, g in (((x, delta, bc), y), (cut, y1)):                 # y as the gradient, then everything back
+        rows = q[0].shape[1]
+        kept = torch.empty(dg.selective_scan_checkpoints(T, rows, f, N), device=DEV)
+        ws = torch.empty(max(dg.selective_scan_workspace(T, rows, f, N), dg.selective_scan_backward_workspace(T, rows, f, N)), dtype=torch.uint8, device=DEV)
+        dg.selective_scan(*q, a, torch.empty_like(q[0]), ws, checkpoints=kept)
+        out = [torch.empty_like(t) for t in q]
+        dg.selective_scan_backward(*q, a, g, kept, *out, torch.empty_like(a), ws)
+        back.append([t[:, -tail:].clone() for t in out])
+        del kept, ws, out
+    assert all(torch.equal(p, q) for p, q in zip(*back))
+    del h, back
     taps = torch.randn((4, f), device=DEV)
     dg.causal_conv(x, taps, None, y, silu=True)
     dg.causal_conv(cut[0], taps, None, y1, silu=True)
     assert torch.equal(y[:, -tail:], y1)
-    del h
     ws = torch.empty(dg.causal_conv_backward_workspace(T, n, f, 4), dtype=torch.uint8, device=DEV)
     dx, dtaps, dx1 = torch.empty_like(x), torch.empty_like(taps), torch.empty_like(y1)
     dg.causal_conv_backward(x, taps, None, delta, dx, dtaps, None, ws, silu=True)
