@@ -697,7 +697,7 @@ int dgnn_add(const void *a, const void *b, void *out, int64_t n, int32_t f, dgnn
  *   x_before [w-1][n][f]   the frames ahead of the series, oldest first, or NULL (zeros)
  *   x_after [w-1][n][f]    receives the last w-1 frames of (x_before, x), or NULL; may be x_before, and no other input or output
  *   flags                  DGNN_SILU or 0
- * Errors: NULL, SHAPE, OVERFLOW (T * n beyond 2^44 too), ALIGN, ALIAS.
+ * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS.
  */
 int dgnn_causal_conv(const void *x, const float *taps, const float *bias, const void *x_before, void *y, void *x_after,
                      const int32_t *lengths, int64_t T, int64_t n, int32_t f, int32_t w, uint32_t flags, dgnn_dtype dt, void *stream);
@@ -730,7 +730,7 @@ int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bia
  *   ws                           dgnn_selective_scan_workspace() bytes, 16-byte aligned
  * States, step sizes and sums are fp32, y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose
  * states are joined afterwards: the same sums in another order.  Results repeat bit for bit.
- * Errors: NULL, SHAPE, OVERFLOW (T * n beyond 2^44 too), ALIGN, ALIAS, CAPACITY.
+ * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS, CAPACITY.
  */
 int dgnn_selective_scan_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
 int dgnn_selective_scan_checkpoints(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
@@ -745,7 +745,7 @@ int dgnn_selective_scan(const void *x, const void *delta, const void *bc, const 
  *   dx, ddelta [T][n][f], dbc [T][n][2 N], dz [T][n][f] (NULL where z is)
  *   da [f][N], dd [f], ddt_bias [f] (NULL where d, dt_bias are) fp32: written, or added to with accumulate != 0
  *   dh_before [n][f][N] fp32 or NULL
- * Sums over channels are fp32, those over time and sequences fp32 over 16 timesteps and 64 bits beyond, all in a fixed order.
+ * Sums over channels are fp32, those over time and sequences fp32 over up to 64 timesteps and 64 bits beyond, all in a fixed order.
  *   ws: dgnn_selective_scan_backward_workspace() bytes.  Outputs overlap neither inputs nor each other.
  */
 int dgnn_selective_scan_backward_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);

@@ -299,7 +299,7 @@ __global__ __launch_bounds__(1024) void conv_sums_kernel(const float *__restrict
 // ---- host ---------------------------------------------------------------------------------------------------------
 int check(int64_t T, int64_t n, int32_t f, int32_t w) {
     if (T <= 0 || n <= 0 || f < 16 || f % 16 || f > DGNN_MAX_CHANNELS || w < 2 || w > 4) return DGNN_ERR_SHAPE;
-    if (!fits_index(n) || !fits_index(T) || T > (int64_t(1) << 44) / n) return DGNN_ERR_OVERFLOW;
+    if (!fits_index(n) || T > (int64_t(1) << 30) || T > (int64_t(1) << 44) / n) return DGNN_ERR_OVERFLOW;   // a place behind the last piece still is an int
     return DGNN_OK;
 }
 

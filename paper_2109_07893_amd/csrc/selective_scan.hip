@@ -35,7 +35,7 @@ constexpr int kWaves = 4;                 // wavefronts of a workgroup of the ke
 // Wavefronts of a workgroup of the adjoint at most, and of all its workgroups: two on a SIMD, and three with 8 states, whose registers
 // allow it (2^17 x 128 fp32: 226 us with two, 193 with three); workgroups of four then, for three times eight do not fit.
 constexpr int back_waves(int states) { return states == 8 ? 4 : 8; }
-constexpr int back_resident(int states) { return states == 8 ? 3072 : 2048; }
+constexpr int back_resident(int states) { return (states == 8 ? 3 : 2) * 4 * 256; }   // of 4 SIMDs on 256 CUs
 constexpr int kMaxGrid = 1 << 22;         // workgroups of a launch: HIP counts its threads in 32 bits
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eLow = 1.92596299112661746887e-8f;
@@ -487,6 +487,12 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
 // what a run does to a state (its own part, its decay) first, then the runs ahead of it one after the other, then its pieces.  Runs are for
 // many pieces of few states (147 of 6144: 7.7 us with sixteen runs, 15 with one; 10 of 98304, which then lie in lines of their own: 24 and 5).
 constexpr int kJoin = 16, kJoinThreads = 256;
+// 2^(time a2) h.  The exponent goes in last: across pieces of a series whose states may grow (a > 0) the factor alone leaves fp32 where the
+// state does not, and no timestep leaves it as it is whatever a is.
+__device__ __forceinline__ float across(float h, float time, float a2) {
+    const float p = time == 0.0f ? 0.0f : fminf(fmaxf(time * a2, -4096.0f), 4096.0f), whole = floorf(p);
+    return ldexpf(h * exp2_of(p - whole), (int)whole);
+}
 template <int STEP, int RUNS> __global__ __launch_bounds__(kJoinThreads) void join_kernel(Scan s, const float *behind, int states) {
     constexpr int STATES = kJoinThreads / RUNS;
     __shared__ float s_part[RUNS][STATES], s_time[RUNS][STATES];
@@ -509,7 +515,7 @@ template <int STEP, int RUNS> __global__ __launch_bounds__(kJoinThreads) void jo
 #pragma unroll
             for (int j = 0; j < kJoin; ++j)
                 if (k + j < k1) {
-                    h = fmaf(exp2_of(step[j] * a2), h, part[j]);
+                    h = across(h, step[j], a2) + part[j];
                     time += step[j];
                     if (store && at < width) s.piece_state[(first + STEP * (k + j)) * width + i] = h;
                 }
@@ -521,7 +527,7 @@ template <int STEP, int RUNS> __global__ __launch_bounds__(kJoinThreads) void jo
         s_part[run][o] = pieces(0.0f, time, false);
         s_time[run][o] = time;
         __syncthreads();
-        for (int r = 0; r < run; ++r) h = fmaf(exp2_of(s_time[r][o] * a2), h, s_part[r][o]);
+        for (int r = 0; r < run; ++r) h = across(h, s_time[r][o], a2) + s_part[r][o];
     }
     pieces(h, time, true);
 }
@@ -925,8 +931,8 @@ bool scan_states(int32_t N) { return N == 8 || N == 16 || N == 32; }
 
 int check_shape(int64_t T, int64_t n, int32_t f, int32_t N) {
     if (T <= 0 || n <= 0 || f < kChannels || f % kChannels || f > DGNN_MAX_CHANNELS || !scan_states(N)) return DGNN_ERR_SHAPE;
-    if (!fits_index(n) || !fits_index(T) || T > (int64_t(1) << 44) / n) return DGNN_ERR_OVERFLOW;
-    return DGNN_OK;
+    if (!fits_index(n) || T > (int64_t(1) << 30) || T > (int64_t(1) << 44) / n) return DGNN_ERR_OVERFLOW;
+    return DGNN_OK;                       // a place behind the last piece still is an int
 }
 
 struct Pieces { int chunk, count; };

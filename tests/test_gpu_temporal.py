@@ -331,6 +331,41 @@ def test_scan_step_sizes(delta):
     s.check()
 
 
+@pytest.mark.parametrize("T", [600, 5000])
+def test_scan_growing_states(T):
+    """a > 0, where the growth across a piece of the time axis is beyond fp32 and no state is: zero until the last timesteps (from behind:
+    until the first ones), which are what they are on their own."""
+    n, f, N, few = 1, 32, 8, 6
+    s = Scan(T, n, f, N, F32, d=False, dt_bias=False, before=False)
+    s.a, s.dh_after = 0.1 * s.a.abs(), None                       # up to e^6 or so a timestep
+    s.x[:-few], s.g_y[few:] = 0.0, 0.0
+
+    def part(lo, hi):
+        b = Scan(few, n, f, N, F32, d=False, dt_bias=False, before=False)
+        b.x, b.delta, b.bc, b.z, b.g_y = (t[lo:hi].clone() for t in (s.x, s.delta, s.bc, s.z, s.g_y))
+        b.a, b.dh_after = s.a, None
+        return b
+
+    y, after, kept = s.forward()
+    y1, after1, _ = part(T - few, T).forward()
+    assert not y[:-few].any() and torch.equal(y[-few:], y1) and torch.equal(after, after1)
+    got = s.backward(kept)
+    first = part(0, few)
+    want = first.backward(first.forward()[2])
+    for k in ("dx", "ddelta", "dbc", "dz"):
+        assert torch.isfinite(got[k]).all() and torch.equal(got[k][:few], want[k]) and not got[k][few:].any(), k
+    assert torch.equal(got["dh_before"], want["dh_before"])
+
+
+@pytest.mark.parametrize("T", [5, 400])
+def test_scan_no_state_kept(T):
+    """a of minus infinity: what a timestep finds is forgotten; a sequence without a timestep keeps its state."""
+    s = Scan(T, 3, 16, 8, F32, lengths=[0, T, 1])
+    s.a[:, ::2] = -float("inf")
+    y, after, _ = s.forward(keep=False)
+    assert torch.equal(after[0], cuda(s.h_before)[0]) and torch.isfinite(y).all() and torch.isfinite(after).all()
+
+
 def test_scan_infinite_values_stay_where_they_are():
     """An infinity or a NaN in one sequence, or in a channel of it, does not reach another."""
     s = Scan(21, 4, 32, 16, F32)

@@ -107,6 +107,13 @@ def test_scan_backward_refusals(lib):
     assert call(dx=AT[0]) == ALIAS and call(ddelta=AT[10]) == ALIAS and call(dh_before=AT[9]) == ALIAS and call(dbc=AT[2]) == ALIAS and call(ws=AT[13]) == ALIAS
 
 
+def test_most_timesteps(lib):
+    """2^30 timesteps at most: positions in time are 32-bit numbers, one piece of the time axis further on too."""
+    for fn, last in (("dgnn_causal_conv_backward_workspace", 4), ("dgnn_selective_scan_workspace", 8), ("dgnn_selective_scan_backward_workspace", 8),
+                     ("dgnn_selective_scan_checkpoints", 8)):
+        assert size(getattr(lib, fn), 1 << 30, 1, 16, last)[0] == 0 and size(getattr(lib, fn), (1 << 30) + 1, 1, 16, last)[0] == OVERFLOW, fn
+
+
 class Item(ctypes.Structure):
     _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dt", ctypes.c_int64)]
 
