@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Tensors t, const d
     const double total = total_of(sums, count, s_sum);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
     const double most = max_norm / (total + 1e-6);
-    const bool clip = isfinite(total) && most < 1.0;         // a norm that is no finite number: nothing to scale by
+    const bool clip = isfinite((float)total) && most < 1.0;  // a norm that *norm shows as no finite number: nothing to scale by
     const float factor = clip ? (float)most : 1.0f;
     while (i >= 0) {
         if (clip || t.out[s.k] != t.g[s.k]) {

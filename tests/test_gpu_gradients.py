@@ -94,6 +94,15 @@ def test_not_finite_changes_nothing(value):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and torch.equal(a.view(torch.uint8), c.view(torch.uint8))
 
 
+def test_norm_beyond_float():
+    """Every gradient is finite, their norm is not in 32 bits: what the caller finds is infinity, and unchanged gradients."""
+    grads = [torch.full((9,), 2e38, device=DEV)]
+    assert float(dg.Gradients(grads).clip(1.0)) == float("inf") and bool((grads[0] == 2e38).all())
+    grads = [torch.full((2,), 2e38, device=DEV)]                    # 2.8e38: still a number
+    dg.Gradients(grads).clip(1.0)
+    assert (grads[0].double() - 0.5 ** 0.5).abs().max() <= 2.0 ** -22
+
+
 def test_refusals():
     g = torch.ones(64, device=DEV)
     for grads, out in (([g, g], None), ([g[:40], g[30:]], None), ([g, torch.ones(64, device=DEV)], [torch.empty(64, device=DEV), g])):
