@@ -44,7 +44,8 @@ class StateSpaceLayer(ClipsGradients):
         self.state = torch.zeros((n, d, states), device=dev)
         self.frames_before = torch.empty_like(self.frames)                             # ... and ahead of the block that backward() is for
         self.ws = torch.empty(B.selective_scan_workspace(T, n, d, states), dtype=torch.uint8, device=dev)
-        self.checkpoints = self.grads = None
+        self.one = [empty(1, n, width) for width in (d, d, d, d, d, 2 * states, f)]    # the same of one timestep: step() leaves the block's alone
+        self.checkpoints = self.grads = self.x = None
 
     def reset(self) -> None:
         """The start of a series: no frames, no state."""
@@ -54,8 +55,8 @@ class StateSpaceLayer(ClipsGradients):
     def _project(self, x: torch.Tensor, name: str, to: torch.Tensor) -> None:
         B.feature_transform(x.reshape(-1, x.shape[-1]), self.weights[name], to.view(-1, to.shape[-1]))
 
-    def _run(self, x: torch.Tensor, rows: slice, lengths, checkpoints) -> torch.Tensor:
-        p, u0, u, z, delta, y, bc, out = self.weights, self.u0[rows], self.u[rows], self.z[rows], self.delta[rows], self.y[rows], self.bc[rows], self.out[rows]
+    def _run(self, x: torch.Tensor, buffers, lengths, checkpoints) -> torch.Tensor:
+        p, (u0, u, z, delta, y, bc, out) = self.weights, buffers
         self._project(x, "w_in", u0)
         self._project(x, "w_z", z)
         B.causal_conv(u0, p["taps"], p["conv_bias"], u, silu=True, x_before=self.frames, x_after=self.frames, lengths=lengths)
@@ -71,19 +72,23 @@ class StateSpaceLayer(ClipsGradients):
             raise ValueError(f"StateSpaceLayer: expected {self.dtype} frames of shape {shape} on {self.dev}")
 
     def forward(self, x: torch.Tensor, train: bool = False) -> torch.Tensor:
-        """The block's output frames [T, n, f] (a buffer of the layer's) from the state as it stands, which moves on to the block's end."""
+        """The block's output frames [T, n, f] (a buffer of the layer's) from the state as it stands, which moves on to the block's end.
+        train: backward() may follow, and looks at x once more."""
         self._check(x, (self.T, self.n, self.f))
+        if x.untyped_storage().data_ptr() == self.out.untyped_storage().data_ptr():
+            raise ValueError("StateSpaceLayer: the frames are the layer's own output buffer")
+        self.x = None
         if train:
             if self.checkpoints is None:
                 self.checkpoints = torch.empty(B.selective_scan_checkpoints(self.T, self.n, self.d, self.states), device=self.dev)
             self.frames_before.copy_(self.frames)
             self.x = x
-        return self._run(x, slice(0, self.T), self.lengths, self.checkpoints if train else None)
+        return self._run(x, (self.u0, self.u, self.z, self.delta, self.y, self.bc, self.out), self.lengths, self.checkpoints if train else None)
 
     def step(self, x: torch.Tensor) -> torch.Tensor:
-        """One timestep further: frames [n, f] in and out."""
+        """One timestep further: frames [n, f] in and out (a buffer of the layer's, which the next step may take in)."""
         self._check(x, (self.n, self.f))
-        return self._run(x[None], slice(0, 1), None, None)[0]
+        return self._run(x[None], self.one, None, None)[0]
 
     def _training_buffers(self) -> None:
         empty = lambda like: torch.empty_like(like)  # noqa: E731
@@ -97,10 +102,12 @@ class StateSpaceLayer(ClipsGradients):
         self.ws_back = torch.empty(max(need), dtype=torch.uint8, device=self.dev)
 
     def backward(self, g_out: torch.Tensor, behind=None, accumulate: bool = False) -> torch.Tensor:
-        """g_out [T, n, f] = dL/d(output frames) of the last forward(train=True); returns dL/dx [T, n, f].  behind = (gradient of the frames,
+        """g_out [T, n, f] = dL/d(output frames) of the last forward(), which was one with train; returns dL/dx [T, n, f].  behind = (gradient of the frames,
         gradient of the state) that the block behind leaves in (dframes, dstate); this one's are there afterwards (pass copies of them
         on to the block ahead of this one, or this layer's own where the blocks share it).  accumulate adds to grads."""
         self._check(g_out, (self.T, self.n, self.f))
+        if self.x is None:
+            raise ValueError("StateSpaceLayer: backward() follows forward(train=True)")
         if self.grads is None:
             self._training_buffers()
         if behind is not None:
@@ -127,4 +134,6 @@ class StateSpaceLayer(ClipsGradients):
         return self.dx
 
     def parameter_gradients(self) -> List[torch.Tensor]:
+        if self.grads is None:
+            raise ValueError("StateSpaceLayer: no backward() so far")
         return list(self.grads.values())

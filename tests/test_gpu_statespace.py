@@ -220,6 +220,36 @@ def test_trainers_clip():
     check_clip(tr, 0.01)
 
 
+def test_steps_between_forward_and_backward():
+    """A model that serves while it is trained: timesteps taken after the block's forward pass leave its outputs and gradients alone."""
+    T, n, f = 6, 9, 16
+    p = make_weights(f, 32, 8, 4)
+    g = torch.Generator().manual_seed(6)
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV), torch.randn((T, n, f), generator=g).to(DEV)
+    plain, served = StateSpaceLayer(n, T, p), StateSpaceLayer(n, T, p)
+    want, want_dx = plain.forward(x, train=True), plain.backward(g_out)
+    out = served.forward(x, train=True)
+    frame = served.step(x[0])
+    for _ in range(2):
+        frame = served.step(frame)                                  # its own output taken in
+    assert torch.equal(out, want) and torch.equal(served.backward(g_out), want_dx)
+    assert all(torch.equal(plain.grads[k], served.grads[k]) for k in plain.grads)
+    again = plain.forward(torch.cat([x[:1], frame[None].expand(T - 1, n, f)]).contiguous())
+    assert torch.isfinite(again).all()
+
+
+def test_backward_needs_its_forward():
+    p = make_weights(16, 32, 8, 4)
+    layer, x = StateSpaceLayer(4, 3, p), torch.zeros((3, 4, 16), device=DEV)
+    for step in (lambda: layer.backward(x), lambda: layer.clip_gradients(1.0), lambda: layer.forward(layer.out, train=True)):
+        with pytest.raises(ValueError):
+            step()
+    layer.forward(x, train=True)
+    layer.forward(x)                                                # the activations are this call's now, its checkpoints were not kept
+    with pytest.raises(ValueError):
+        layer.backward(x)
+
+
 def test_refusals():
     p = make_weights(16, 32, 8, 4)
     with pytest.raises(ValueError):
