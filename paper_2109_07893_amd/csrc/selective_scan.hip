@@ -219,7 +219,11 @@ struct Place {
     int64_t v;
     int p, t0, t1, t_end;
     __device__ __forceinline__ bool settle(const Scan &s, int pieces) {          // after v was moved on
-        while (v >= s.n) { v -= s.n; ++p; }
+        if (v >= s.n) {                   // both below 2^32; one step at a time, many pieces of one sequence took 30 us to count
+            const uint32_t on = (uint32_t)v / (uint32_t)s.n;
+            v -= (int64_t)on * s.n;
+            p += (int)on;
+        }
         if (p >= pieces) return false;
         t0 = p * s.chunk;
         t1 = min(s.T, t0 + s.chunk);
@@ -483,53 +487,61 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
 
 // The states between the pieces, in place.  Forward (STEP 1): piece p left part[p] behind when it started from zero, part[0] from h_before;
 // the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
-// reaches piece p from behind takes the place p + 1.  A thread has one state of one of RUNS runs of pieces, kJoin of them fetched together:
-// what a run does to a state (its own part, its decay) first, then the runs ahead of it one after the other, then its pieces.  Runs are for
-// many pieces of few states (147 of 6144: 7.7 us with sixteen runs, 15 with one; 10 of 98304, which then lie in lines of their own: 24 and 5).
-constexpr int kJoin = 16, kJoinThreads = 256;
+// reaches piece p from behind takes the place p + 1.  A thread has one state of one of RUNS runs of at most kJoin pieces, which are fetched
+// together: what a run does to a state (its own part, its decay) first, then the same of all runs up to each, twice as many with every step,
+// then its pieces.
+constexpr int kJoin = 16, kJoinRuns = 32;
+constexpr int join_states(int runs) { return runs == 1 ? 256 : runs == 4 ? 64 : 32; }         // of a workgroup
 // 2^(time a2) h.  The exponent goes in last: across pieces of a series whose states may grow (a > 0) the factor alone leaves fp32 where the
 // state does not, and no timestep leaves it as it is whatever a is.
 __device__ __forceinline__ float across(float h, float time, float a2) {
     const float p = time == 0.0f ? 0.0f : fminf(fmaxf(time * a2, -4096.0f), 4096.0f), whole = floorf(p);
     return ldexpf(h * exp2_of(p - whole), (int)whole);
 }
-template <int STEP, int RUNS> __global__ __launch_bounds__(kJoinThreads) void join_kernel(Scan s, const float *behind, int states) {
-    constexpr int STATES = kJoinThreads / RUNS;
+template <int STEP, int RUNS> __global__ __launch_bounds__(RUNS *join_states(RUNS)) void join_kernel(Scan s, const float *behind, uint32_t states) {
+    constexpr int STATES = join_states(RUNS);
     __shared__ float s_part[RUNS][STATES], s_time[RUNS][STATES];
-    const int64_t width = s.n * s.f * states;                                // a multiple of sixteen; beyond it: its last state once more
+    // Series in pieces are few: a place among the states of all of them is a 32-bit number.  Beyond the last state: that one once more.
+    const uint32_t channels = (uint32_t)s.n * (uint32_t)s.f, width = channels * states;
     const int o = threadIdx.x % STATES, run = threadIdx.x / STATES;
-    const int64_t at = (int64_t)blockIdx.x * STATES + o, i = min(at, width - 1), c = i / states;
-    const float a2 = s.a[c % s.f * states + i % states] * kLog2e;
+    const uint32_t at = blockIdx.x * STATES + o, i = min(at, width - 1), c = i / states;
+    const float a2 = s.a[i % ((uint32_t)s.f * states)] * kLog2e;
     const int first = STEP > 0 ? 1 : s.pieces - 1, count = s.pieces - (STEP > 0 ? 2 : 1), per = (count + RUNS - 1) / RUNS;
     const int k0 = run * per, k1 = min(count, k0 + per);
-    auto pieces = [&](float h, float &time, bool store) {
-        time = 0.0f;
-        for (int k = k0; k < k1; k += kJoin) {
-            float part[kJoin], step[kJoin];
+    float part[kJoin], step[kJoin];
 #pragma unroll
-            for (int j = 0; j < kJoin; ++j) {
-                const int p = first + STEP * min(k + j, k1 - 1);
-                part[j] = s.piece_state[p * width + i];
-                step[j] = s.piece_time[p * s.n * s.f + c];
-            }
-#pragma unroll
-            for (int j = 0; j < kJoin; ++j)
-                if (k + j < k1) {
-                    h = across(h, step[j], a2) + part[j];
-                    time += step[j];
-                    if (store && at < width) s.piece_state[(first + STEP * (k + j)) * width + i] = h;
-                }
-        }
-        return h;
-    };
-    float time, h = STEP > 0 ? s.piece_state[i] : behind ? behind[i] : 0.0f;
+    for (int j = 0; j < kJoin; ++j) {
+        const uint64_t p = first + STEP * min(k0 + j, count - 1);
+        part[j] = s.piece_state[p * width + i];
+        step[j] = s.piece_time[p * channels + c];
+    }
+    float h = STEP > 0 ? s.piece_state[i] : behind ? behind[i] : 0.0f;
     if (RUNS > 1) {
-        s_part[run][o] = pieces(0.0f, time, false);
+        float own = 0.0f, time = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j)
+            if (k0 + j < k1) { own = across(own, step[j], a2) + part[j]; time += step[j]; }
+#pragma unroll
+        for (int d = 1; d < RUNS; d <<= 1) {
+            s_part[run][o] = own;
+            s_time[run][o] = time;
+            __syncthreads();
+            const float before = run >= d ? s_part[run - d][o] : 0.0f, time_before = run >= d ? s_time[run - d][o] : 0.0f;
+            __syncthreads();
+            own += across(before, time, a2);
+            time += time_before;
+        }
+        s_part[run][o] = own;
         s_time[run][o] = time;
         __syncthreads();
-        for (int r = 0; r < run; ++r) h = across(h, s_time[r][o], a2) + s_part[r][o];
+        if (run > 0) h = across(h, s_time[run - 1][o], a2) + s_part[run - 1][o];
     }
-    pieces(h, time, true);
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j)
+        if (k0 + j < k1) {
+            h = across(h, step[j], a2) + part[j];
+            if (at < width) s.piece_state[(uint64_t)(first + STEP * (k0 + j)) * width + i] = h;
+        }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
@@ -937,15 +949,21 @@ int check_shape(int64_t T, int64_t n, int32_t f, int32_t N) {
 
 struct Pieces { int chunk, count; };
 
-Pieces pieces_of(int64_t T, int64_t items, int64_t wanted) {
+// The time axis in pieces of whole tiles where there is less work across it than the device holds: `items` walks side by side (going ahead a wavefront's,
+// going back a workgroup's) out of `wanted`.  Every piece is walked twice, so going ahead fewer than four do not pay (2^17 x 128 channels, two pieces: 226
+// us against 198); going back, where the first walk is a quarter of the second, two do (128 sequences of 256 x 128: 106 us against 140).
+// The fewest timesteps weigh the second walk against the launches: 64 ahead (80 of 16 sequences 10.9 us against 11.9, 64 of them 12.2 against
+// 11.1), 32 back (48 of two: 20 against 29 us, 32 of a hundred: 24.7 against 22.6).  Twice as many tiles to a piece cost 10 - 20 % at a few hundred
+// timesteps (16 sequences of 128 x 64: 14.5 us for 12.1); no more pieces than one join takes.
+Pieces pieces_of(int64_t T, int64_t items, int64_t wanted, int64_t least, int64_t least_tiles) {
     const int64_t tiles = (T + kTile - 1) / kTile;
-    int64_t count = std::min<int64_t>(tiles / 2, wanted / std::max<int64_t>(items, 1));
-    if (count < 4) return {(int)(tiles * kTile), 1};
+    const int64_t count = std::min<int64_t>({tiles, wanted / items, kJoinRuns * kJoin});
+    if (count < least || tiles < least_tiles) return {(int)(tiles * kTile), 1};
     const int64_t chunk = (tiles + count - 1) / count * kTile;
     return {(int)chunk, (int)((T + chunk - 1) / chunk)};
 }
 
-Pieces forward_pieces(int64_t T, int64_t n, int32_t f) { return pieces_of(T, n * (f / kChannels), 4096); }
+Pieces forward_pieces(int64_t T, int64_t n, int32_t f) { return pieces_of(T, n * (f / kChannels), 4096, 4, 5); }
 
 struct BackShape { int groups, blocks_of_groups, waves; Pieces pieces; int64_t slots; };
 
@@ -955,7 +973,7 @@ BackShape back_shape(int64_t T, int64_t n, int32_t f, int32_t N) {
     b.blocks_of_groups = (b.groups + back_waves(N) - 1) / back_waves(N);
     b.waves = std::min(b.groups, back_waves(N));
     const int64_t blocks = std::max(1, back_resident(N) / (b.waves * b.blocks_of_groups));
-    b.pieces = pieces_of(T, n, blocks);
+    b.pieces = pieces_of(T, n, blocks, 2, 3);
     b.slots = std::min<int64_t>(n * b.pieces.count, blocks);
     return b;
 }
@@ -993,8 +1011,13 @@ template <typename F> int by_kind(dgnn_dtype dt, int32_t N, F &&launch) {
 
 template <int STEP> int join_pieces(const Scan &s, const float *behind, int32_t states, hipStream_t st) {
     const int64_t width = s.n * s.f * states;
-    if (s.pieces > 2 * kJoin) hipLaunchKernelGGL((join_kernel<STEP, 16>), dim3((unsigned)(width / 16)), dim3(kJoinThreads), 0, st, s, behind, states);
-    else hipLaunchKernelGGL((join_kernel<STEP, 1>), dim3((unsigned)((width + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st, s, behind, states);
+    auto launch = [&](auto runs) {
+        constexpr int RUNS = decltype(runs)::value, STATES = join_states(RUNS);
+        hipLaunchKernelGGL((join_kernel<STEP, RUNS>), dim3((unsigned)((width + STATES - 1) / STATES)), dim3(RUNS * STATES), 0, st, s, behind, (uint32_t)states);
+    };
+    if (s.pieces > 4 * kJoin) launch(std::integral_constant<int, kJoinRuns>{});
+    else if (s.pieces > kJoin) launch(std::integral_constant<int, 4>{});
+    else launch(std::integral_constant<int, 1>{});
     DGNN_RETURN_IF_LAUNCH_FAILED();
     return DGNN_OK;
 }
