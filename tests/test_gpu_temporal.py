@@ -450,3 +450,50 @@ def test_another_stream_and_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, results))
         s.forward()
+
+
+def test_two_streams_and_two_graphs():
+    """Two series at once, each on a stream and in a workspace of its own; then a graph of each over ONE workspace, replayed in turn."""
+    runs = [Scan(300, 2, 48, 16, F32, seed=1), Scan(500, 1, 32, 8, BF16, seed=2)]
+    size = max(max(dg.selective_scan_workspace(s.T, s.n, s.f, s.N), dg.selective_scan_backward_workspace(s.T, s.n, s.f, s.N)) for s in runs)
+    spaces = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in runs]
+
+    def prepared(s):
+        i = s.inputs()
+        out = {k: torch.empty_like(i[k[1:]]) for k in ("dx", "ddelta", "dbc", "dz", "da", "dd", "ddt_bias")}
+        return i, out, torch.empty_like(i["x"]), torch.empty(dg.selective_scan_checkpoints(s.T, s.n, s.f, s.N), device=DEV), cuda(s.g_y)
+
+    sets = [prepared(s) for s in runs]
+
+    def work(k, ws):
+        i, out, y, kept, g_y = sets[k]
+        dg.selective_scan(y=y, ws=ws, checkpoints=kept, **i)
+        dg.selective_scan_backward(g_y=g_y, checkpoints=kept, ws=ws, **i, **out)
+
+    for k in range(2):
+        work(k, spaces[k])
+    eager = [[y.clone()] + [t.clone() for t in out.values()] for _, out, y, _, _ in sets]
+    streams = [torch.cuda.Stream() for _ in runs]
+
+    def check():
+        torch.cuda.synchronize()
+        for want, (_, out, y, _, _) in zip(eager, sets):
+            assert all(torch.equal(a, b) for a, b in zip(want, [y] + list(out.values())))
+            for t in [y] + list(out.values()):
+                t.zero_()
+        torch.cuda.synchronize()
+
+    check()
+    for _ in range(3):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                work(k, spaces[k])
+        check()
+    graphs = [torch.cuda.CUDAGraph() for _ in runs]
+    for k, graph in enumerate(graphs):
+        with torch.cuda.graph(graph):
+            work(k, spaces[0])
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        check()
