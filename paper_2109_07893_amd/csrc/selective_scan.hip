@@ -30,7 +30,9 @@ using namespace dgnn;
 
 constexpr int kChannels = 16;             // channels of a wavefront
 constexpr int kTile = 16;                 // timesteps of a tile
-constexpr int kHeld = 8;                  // ... between two kept states: the adjoint holds the states of so many in registers
+// ... between two kept states: the adjoint holds the states of so many timesteps in registers (sixteen would be 32 registers more with 16 states,
+// which spill); the forward pass writes 4 N / 8 bytes a value for them.
+constexpr int kHeld = 8;
 constexpr int kWaves = 4;                 // wavefronts of a workgroup of the kernels without sums over channels
 // Wavefronts of a workgroup of the adjoint at most, and of all its workgroups: two on a SIMD, and three with 8 states, whose registers
 // allow it (2^17 x 128 fp32: 226 us with two, 193 with three); workgroups of four then, for three times eight do not fit.
@@ -271,6 +273,10 @@ template <bool BF16, int S, int K> struct Rows {
 };
 
 // ---- forward ------------------------------------------------------------------------------------------------------
+// What bounds it: vector instructions, then memory.  A state takes five a timestep (two products, the exponential, which holds the pipe for
+// two, two multiply-adds), a lane's four 24 slots of some 34; the rest is the step sizes (25 instructions for four timesteps), the exchange of
+// four timesteps' sums (9), the gate, addresses.  16 x 100003 x 64 fp32, 16 states, gated: 590 us, vector instructions in 79 % of the cycles at
+// four wavefronts per SIMD (114 registers), 3.8 TB/s of the 4.8 that a copy reaches; bf16 at half the bytes takes the same.
 template <bool BF16, int S> struct Tile {
     Rows<BF16, S, kTile> rows;
     float x[kTile / 4], delta[kTile / 4], z[kTile / 4], h[S];
@@ -286,7 +292,9 @@ __device__ __forceinline__ void load_tile(Tile<BF16, S> &r, const Scan &s, const
         r.delta[i] = Elem<BF16>::get(static_cast<const E *>(s.delta) + first_at + i * four);
         if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + first_at + i * four);
     };
-    if (S <= 4 && steps == kTile) {       // no lane stands aside: nothing for the compiler to wait for ahead of the loads (4 - 7 %; with 32 states it costs that)
+    // No lane stands aside in a whole tile: nothing for the compiler to wait for ahead of the loads (4 - 7 %, 16 x 8192 x 128 bf16 with 32 states 148
+    // us against 159; with 32 states in fp32, whose rows take twice the registers, it costs that).
+    if ((S <= 4 || BF16) && steps == kTile) {
         r.rows.load_all(s.bc, s.n, v, t, kTile, l.lane);
 #pragma unroll
         for (int i = 0; i < kTile / 4; ++i) values(i);
@@ -434,14 +442,16 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
     __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
     scan_tiles<BF16, S, true, GATE>(s, s_rows);
 }
-// Where there are few sequences the time axis is cut into pieces, and this goes ahead over all but the last one.
+// Where there are few sequences the time axis is cut into pieces, and this goes ahead over all but the last one: 3 x 16411 x 128 bf16 in 147
+// pieces takes 31 us here, 7 to join and 40 for the outputs, where one wavefront per sixteen channels would walk 1026 tiles, 2 us each.
 template <bool BF16, int S> __global__ __launch_bounds__(kWaves *kWave) void scan_piece_kernel(Scan s) {
     __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
     scan_tiles<BF16, S, false, false>(s, s_rows);
 }
 
 // One timestep, the step of a model that follows a running series: a wavefront per sixteen channels of a sequence and no more.  The state
-// comes and goes (8 N bytes a channel against 4 x 2 or 4 of everything else), and what streams it is many wavefronts that are soon done.
+// comes and goes (8 N bytes a channel against 4 x 2 or 4 of everything else), and what streams it is many wavefronts that are soon done:
+// 100000 x 128 fp32 350 us against 479 by the kernel that walks, 16 x 128 3.5 against 4.7.  60013 x 64 bf16: 107 us, 4.9 TB/s.
 template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWave) void scan_step_kernel(Scan s) {
     typedef typename Elem<BF16>::Type E;
     constexpr int N = 4 * S;
@@ -489,7 +499,9 @@ template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWav
 // the state ahead of piece p takes the place p - 1.  Backward (STEP -1): the same from the last piece on, which dh_after reaches; what
 // reaches piece p from behind takes the place p + 1.  A thread has one state of one of RUNS runs of at most kJoin pieces, which are fetched
 // together: what a run does to a state (its own part, its decay) first, then the same of all runs up to each, twice as many with every step,
-// then its pieces.
+// then its pieces.  147 pieces of 6144 states: 7 us; the memory trips (the pieces' states come from other dies' wavefronts) are what it takes.
+// As few runs as hold the pieces: loads that a run has no piece for cost as much as others (16 sequences of 4096 x 128 in 32 pieces: 80 us with
+// four runs, 93 with 32; 128 of 64 x 128 in two: 36 with one, 43 with four).
 constexpr int kJoin = 16, kJoinRuns = 32;
 constexpr int join_states(int runs) { return runs == 1 ? 256 : runs == 4 ? 64 : 32; }         // of a workgroup
 // 2^(time a2) h.  The exponent goes in last: across pieces of a series whose states may grow (a > 0) the factor alone leaves fp32 where the
@@ -545,7 +557,8 @@ template <int STEP, int RUNS> __global__ __launch_bounds__(RUNS *join_states(RUN
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
-// dL/dh as a piece hands it to its predecessor when nothing reaches it from behind, and the sum of its step sizes.
+// dL/dh as a piece hands it to its predecessor when nothing reaches it from behind, and the sum of its step sizes (4 x 1025 x 1536 bf16: 40 us
+// against the 112 of the kernel below).
 template <bool BF16, int S>
 __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
@@ -618,14 +631,13 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
     }
 }
 
-// Timesteps of a tile of the adjoint: what a wavefront fetches ahead.
+// Timesteps of a tile of the adjoint: what a wavefront fetches ahead.  Sixteen where the registers hold them (64 sequences of 1024 x 128 bf16: 181 us
+// against 189 with eight; with 8 states, at three wavefronts per SIMD, 188 with eight and 200 with sixteen; with 32 they spill).
 template <int S> constexpr int kBackTile = S == 4 ? 16 : 8;
 // Whether a tile's loads are all made, whatever is there of it.  With 32 states, where the registers are short, the loads that a branch may
-// pass over cost more (2^17 x 128 fp32: 922 us against 658); with 16 and 8 the addresses that take the branches' place do (338 against 382,
-// 233 against 255).
-template <int S> constexpr bool kAllLoads = S > 4;
-// Decays that a lane keeps in LDS on the way ahead for the way back.
-template <int S> constexpr int kDecays = S <= 4 ? kHeld * S : 0;
+// pass over cost more (2^17 x 128 fp32: 922 us against 658), and with 16 in bf16 (256 x 512 x 128: 303 against 272); with 16 in fp32 the
+// addresses that take the branches' place do where half of a tile is there (7 x 20000 x 64: 230 against 209; 16 x 8192 x 128: 281 against 278), and with 8 neither.
+template <bool BF16, int S> constexpr bool kAllLoads = S > 4 || (BF16 && S == 4);
 
 template <bool BF16, int S> struct BackTile {
     static constexpr int K = kBackTile<S>;
@@ -646,7 +658,7 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanB
         r.gy[i] = Elem<BF16>::get(static_cast<const E *>(b.g_y) + at);
         if (GATE) r.z[i] = Elem<BF16>::get(static_cast<const E *>(s.z) + at);
     };
-    if (kAllLoads<S>) {
+    if (kAllLoads<BF16, S>) {
         steps = min(max(steps, 1), K);
         r.rows.load_all(s.bc, s.n, p.v, t, steps, l.lane);
 #pragma unroll
@@ -669,15 +681,22 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanB
         for (int i = 0; i < S; ++i) r.k[i] = 0.0f;
 }
 
-// A workgroup has all channels of a sequence, or a part of them (of back_waves() wavefronts).
+// A workgroup has all channels of a sequence, or a part of them (of back_waves() wavefronts).  Eight timesteps are walked ahead from a kept state
+// (five instructions a state and timestep) and back again (eight, and 4 for the sums over channels): some 108 a timestep and lane with 16
+// states, and they are what bounds it: 16 x 50021 x 32 fp32 takes 425 us with vector instructions in 80 % of the cycles at two wavefronts per SIMD, 2.9
+// TB/s with the forward pass.  The exchange over channels is 16 of them, its cost when left out 19 %; the matrix cores would take the sums at the same number of
+// issue slots.  16 x 8192 x 128 fp32: 188 us with 8 states, 279 with 16; 16 x 4096 x 128 with 32: 289, bf16 267.
 template <bool BF16, int S, bool GATE>
 __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
     constexpr int N = 4 * S, K = kBackTile<S>, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
     constexpr int J = S <= 4 ? 4 : 2;                                     // timesteps whose sums over channels are exchanged together
+    // With 32 states in fp32 what two fours have in flight together does not fit the registers: they stay apart (16 x 4096 x 128: 291 us against 334);
+    // in bf16 it does (253 against 277).
+    constexpr bool kFence = S > 4 && !BF16;
     // [3][wavefronts][V], the three by turns: B and C of a tile, where dB and dC take their place timestep by timestep (the next tile's B
-    // and C are laid down when a slower wavefront may still be adding up this one's dB and dC); [wavefronts][kHeld][lanes][S] decays where
-    // they fit (17 KB a wavefront with 16 states), which take a product and an exponential each to form again; 64-bit sums.
+    // and C are laid down when a slower wavefront may still be adding up this one's dB and dC); 64-bit sums.  Decays are formed twice: kept here
+    // on the way ahead they took 2 - 4 % longer.
     extern __shared__ float s_mem[];
     const Scan &s = b.s;
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -688,8 +707,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
     const int q = l.q, turn = waves * V;
     float a2[S], acc[S + 2];                                              // sums over a few tiles: da of the lane's states, dd, ddt_bias
     load_decay(a2, s.a, l.ch, q);
-    float *const decays = s_mem + 3 * turn + wave * kDecays<S> * kWave + lane * S;
-    double *const sums = reinterpret_cast<double *>(s_mem + 3 * turn + waves * kDecays<S> * kWave) + wave * (S + 2) * kWave + lane;
+    double *const sums = reinterpret_cast<double *>(s_mem + 3 * turn) + wave * (S + 2) * kWave + lane;
 #pragma unroll
     for (int i = 0; i < S + 2; ++i) { sums[i * kWave] = 0.0; acc[i] = 0.0f; }
     const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f, d = s.d ? s.d[l.ch] : 0.0f;
@@ -707,7 +725,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
     float x[R], dt[R], sig[R], gp[R], gz[R], h0[K / kHeld][S], k[S], from_behind[S];
     BackTile<BF16, S> r;
     auto take = [&](int steps, float *to) {
-        r.rows.template stage<kAllLoads<S>>(to, lane, steps);
+        r.rows.template stage<kAllLoads<BF16, S>>(to, lane, steps);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             x[i] = r.x[i];
@@ -760,16 +778,13 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
                 float rb[S], rc[S];
                 load_state(rb, row + q * S);
                 if (GATE) load_state(rc, row + N + q * S);
-                float e[S];
                 part_y[j] = 0.0f;
 #pragma unroll
                 for (int m = 0; m < S; ++m) {
                     held[(4 * i + j) % kHeld][m] = h[m];
-                    e[m] = exp2_of(dt_j * a2[m]);
-                    h[m] = fmaf(e[m], h[m], dtx_j * rb[m]);
+                    h[m] = fmaf(exp2_of(dt_j * a2[m]), h[m], dtx_j * rb[m]);
                     if (GATE) part_y[j] = fmaf(rc[m], h[m], part_y[j]);
                 }
-                if (kDecays<S>) store_state(decays + (4 * i + j) % kHeld * kWave * S, e);
             };
             step(0, of_lane<0>(dt[i]), of_lane<0>(dtx));
             step(1, of_lane<1>(dt[i]), of_lane<1>(dtx));
@@ -779,7 +794,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
                 const float dz = gz[i] * fmaf(d, x[i], quad_sums(part_y, q));
                 if (decltype(whole)::value || 4 * i + q < steps) Elem<BF16>::put(static_cast<E *>(b.dz) + at + i * four, dz);
             }
-            if (S > 4) __builtin_amdgcn_sched_barrier(0);                 // what the fours have in flight together does not fit the registers
+            if (kFence) __builtin_amdgcn_sched_barrier(0);
         };
         auto back = [&](auto whole, int i) {          // ... and back over them
             float bc[J * 2 * S], ghb[4], sa[4];
@@ -789,8 +804,6 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
                 float rb[S], rc[S];
                 load_state(rb, row + q * S);
                 load_state(rc, row + N + q * S);
-                float e[S];
-                if (kDecays<S>) load_state(e, decays + (4 * i + j) % kHeld * kWave * S);
                 ghb[j] = sa[j] = 0.0f;
 #pragma unroll
                 for (int m = 0; m < S; ++m) {
@@ -799,7 +812,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
                     bc[j % J * 2 * S + S + m] = h[m] * g_j;
                     ghb[j] = fmaf(gh, rb[m], ghb[j]);
                     h[m] = held[(4 * i + j) % kHeld][m];
-                    k[m] = gh * (kDecays<S> ? e[m] : exp2_of(dt_j * a2[m]));
+                    k[m] = gh * exp2_of(dt_j * a2[m]);
                     const float u = k[m] * h[m];
                     sa[j] = fmaf(u, a2[m], sa[j]);
                     acc[m] = fmaf(u, dt_j, acc[m]);
@@ -825,7 +838,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
                 acc[S] = fmaf(gp[i], x[i], acc[S]);
                 acc[S + 1] += ddelta;
             }
-            if (S > 4) __builtin_amdgcn_sched_barrier(0);
+            if (kFence) __builtin_amdgcn_sched_barrier(0);
         };
         auto start = [&](int half) {
 #pragma unroll
@@ -1142,7 +1155,7 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
     }
     int rc = by_kind(dt, states, [&](auto bf16, auto per) {
         constexpr int S = decltype(per)::value;
-        const unsigned lds = shape.waves * ((3u * kBackTile<S> * 8 * S + kDecays<S> * kWave) * sizeof(float) + (S + 2) * kWave * sizeof(double));
+        const unsigned lds = shape.waves * (3u * kBackTile<S> * 8 * S * sizeof(float) + (S + 2) * kWave * sizeof(double));
         const auto kernel = z ? scan_back_kernel<decltype(bf16)::value, S, true> : scan_back_kernel<decltype(bf16)::value, S, false>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(shape.slots * shape.blocks_of_groups)), dim3(shape.waves * kWave), lds, st, b);
     });
