@@ -13,7 +13,7 @@
 // whose timestep they are.  Sums over channels (dB, dC) run across the sixteen groups of four, again many at a time, so that every step
 // of the exchange halves the number of registers; the wavefronts of a sequence then meet in LDS.
 //
-// The time axis goes by tiles of sixteen steps.  B and C of a tile are the same for all channels: a wavefront fetches them as whole
+// The time axis goes by tiles of sixteen steps (eight in short series).  B and C of a tile are the same for all channels: a wavefront fetches them as whole
 // 16-byte pieces and reads them back from LDS, four addresses a read, where a load per timestep would keep the 64 lanes of the
 // cache's port busy for 64 bytes.  Wavefronts stay, keep their channels (and so a, d and the bias) and take one sequence after the other;
 // the loads of the next tile, be it of the next sequence, are under way while a tile is computed.
@@ -29,7 +29,8 @@ namespace {
 using namespace dgnn;
 
 constexpr int kChannels = 16;             // channels of a wavefront
-constexpr int kTile = 16;                 // timesteps of a tile
+constexpr int kTile = 16;                 // timesteps of a tile, but for short series
+constexpr int kPiece = 16;                // ... of a piece of the time axis, at least; pieces are multiples of it
 // ... between two kept states: the adjoint holds the states of so many timesteps in registers (sixteen would be 32 registers more with 16 states,
 // which spill); the forward pass writes 4 N / 8 bytes a value for them.
 constexpr int kHeld = 8;
@@ -51,7 +52,7 @@ struct Scan {
     const int32_t *lengths;
     int64_t n;
     int T, f, groups;                     // groups of kChannels channels
-    int chunk, pieces;                    // the time axis in `pieces` pieces of `chunk` timesteps, a multiple of kTile
+    int chunk, pieces;                    // the time axis in `pieces` pieces of `chunk` timesteps, a multiple of kPiece
     float *piece_state, *piece_time;      // [pieces][n][f][N], [pieces][n][f]
 };
 
@@ -275,16 +276,16 @@ template <bool BF16, int S, int K> struct Rows {
 // ---- forward ------------------------------------------------------------------------------------------------------
 // What bounds it: vector instructions, then memory.  A state takes five a timestep (two products, the exponential, which holds the pipe for
 // two, two multiply-adds), a lane's four 24 slots of some 34; the rest is the step sizes (25 instructions for four timesteps), the exchange of
-// four timesteps' sums (9), the gate, addresses.  16 x 100003 x 64 fp32, 16 states, gated: 590 us, vector instructions in 79 % of the cycles at
-// four wavefronts per SIMD (114 registers), 3.8 TB/s of the 4.8 that a copy reaches; bf16 at half the bytes takes the same.
-template <bool BF16, int S> struct Tile {
-    Rows<BF16, S, kTile> rows;
-    float x[kTile / 4], delta[kTile / 4], z[kTile / 4], h[S];
+// four timesteps' sums (9), the gate, addresses.  16 x 100003 x 64 fp32, 16 states, gated: 568 us, vector instructions in 81 % of the cycles at
+// five wavefronts per SIMD, 4.0 TB/s of the 4.8 that a copy reaches; bf16 at half the bytes takes the same.
+template <bool BF16, int S, int K> struct Tile {
+    Rows<BF16, S, K> rows;
+    float x[K / 4], delta[K / 4], z[K / 4], h[S];
 };
 
 // The tile of `steps` timesteps from t on; the state ahead of it where it is the first one of a series that is not cut into pieces.
-template <bool BF16, int S, bool Y, bool GATE>
-__device__ __forceinline__ void load_tile(Tile<BF16, S> &r, const Scan &s, const Lane<S> &l, int64_t v, int t, int steps, bool first) {
+template <bool BF16, int S, int K, bool Y, bool GATE>
+__device__ __forceinline__ void load_tile(Tile<BF16, S, K> &r, const Scan &s, const Lane<S> &l, int64_t v, int t, int steps, bool first) {
     typedef typename Elem<BF16>::Type E;
     const int64_t first_at = l.at(v, t), four = 4 * s.n * s.f;
     auto values = [&](int i) {
@@ -294,14 +295,14 @@ __device__ __forceinline__ void load_tile(Tile<BF16, S> &r, const Scan &s, const
     };
     // No lane stands aside in a whole tile: nothing for the compiler to wait for ahead of the loads (4 - 7 %, 16 x 8192 x 128 bf16 with 32 states 148
     // us against 159; with 32 states in fp32, whose rows take twice the registers, it costs that).
-    if ((S <= 4 || BF16) && steps == kTile) {
-        r.rows.load_all(s.bc, s.n, v, t, kTile, l.lane);
+    if ((S <= 4 || BF16) && steps == K) {
+        r.rows.load_all(s.bc, s.n, v, t, K, l.lane);
 #pragma unroll
-        for (int i = 0; i < kTile / 4; ++i) values(i);
+        for (int i = 0; i < K / 4; ++i) values(i);
     } else {
         r.rows.load(s.bc, s.n, v, t, steps, l.lane);
 #pragma unroll
-        for (int i = 0; i < kTile / 4; ++i)
+        for (int i = 0; i < K / 4; ++i)
             if (4 * i + l.q < steps) values(i);
     }
     if (first && s.h_before && (Y ? s.pieces == 1 : t == 0)) load_state(r.h, s.h_before + l.state(0, v));
@@ -326,13 +327,13 @@ __device__ __forceinline__ float one_step(float (&h)[S], const float (&a2)[S], c
 
 // Y: outputs are formed (GATE: under z).  Else only what a piece of the time axis leaves behind when it starts from zero (the first: from h_before), and
 // the sum of its step sizes, which gives the decay across it, exp(a sum dt).
-template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void scan_tiles(const Scan &s, float *s_rows) {
+template <bool BF16, int S, int K, bool Y, bool GATE> __device__ __forceinline__ void scan_tiles(const Scan &s, float *s_rows) {
     typedef typename Elem<BF16>::Type E;
     constexpr int N = 4 * S;
     const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), pieces = Y ? s.pieces : s.pieces - 1;
     const int w = blockIdx.x * kWaves + wave, stride = (int)(gridDim.x * kWaves) / s.groups;
     if (w / s.groups >= stride) return;
-    float *const rows = s_rows + wave * 2 * kTile * 2 * N;
+    float *const rows = s_rows + wave * 2 * K * 2 * N;
     const Lane<S> l(s, w % s.groups, lane);
     float a2[S], h[S], time = 0.0f;
     load_decay(a2, s.a, l.ch, l.q);
@@ -343,12 +344,12 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
     // Loads of a tile -> what is computed with.  Loads and stores leave a wavefront in one order and are counted in it, so waiting for a
     // load is waiting for every store ahead of it too: the next tile's loads go out first, are taken up after all of this tile's arithmetic,
     // and this tile's stores follow.
-    Tile<BF16, S> r;
-    float x[kTile / 4], z[kTile / 4], dt[kTile / 4], start[S];
+    Tile<BF16, S, K> r;
+    float x[K / 4], z[K / 4], dt[K / 4], start[S];
     auto take = [&](int steps, int to) {
-        r.rows.template stage<false>(rows + to * kTile * 2 * N, lane, steps);
+        r.rows.template stage<false>(rows + to * K * 2 * N, lane, steps);
 #pragma unroll
-        for (int i = 0; i < kTile / 4; ++i)
+        for (int i = 0; i < K / 4; ++i)
             if (4 * i < steps) {
                 float sig;
                 x[i] = r.x[i];
@@ -358,12 +359,12 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
 #pragma unroll
         for (int k = 0; k < S; ++k) start[k] = r.h[k];
     };
-    load_tile<BF16, S, Y, GATE>(r, s, l, here.v, t, min(kTile, here.t_end - t), true);
-    take(min(kTile, here.t_end - t), 0);
+    load_tile<BF16, S, K, Y, GATE>(r, s, l, here.v, t, min(K, here.t_end - t), true);
+    take(min(K, here.t_end - t), 0);
     for (;;) {
-        const int steps = min(kTile, here.t_end - t);
+        const int steps = min(K, here.t_end - t);
         Place next = here;
-        int t_next = t + kTile;
+        int t_next = t + K;
         bool more = true;
         if (t_next >= here.t_end) {
             next.v += stride;
@@ -382,13 +383,13 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
             time = 0.0f;
         }
         if (Y && s.checkpoints && steps > 0) store_state(s.checkpoints + l.state(t / kHeld, here.v), h);
-        if (more) load_tile<BF16, S, Y, GATE>(r, s, l, next.v, t_next, min(kTile, next.t_end - t_next), t_next == next.t0);
+        if (more) load_tile<BF16, S, K, Y, GATE>(r, s, l, next.v, t_next, min(K, next.t_end - t_next), t_next == next.t0);
         wave_lds_sync();
-        float y[kTile / 4], half[S];
+        float y[K / 4], half[S];
         auto group = [&](int i, int left) {                 // four timesteps, of which `left` are there
-            const float *const row = rows + buffer * kTile * 2 * N + 4 * i * 2 * N + l.q * S;
+            const float *const row = rows + buffer * K * 2 * N + 4 * i * 2 * N + l.q * S;
             const float dtx = dt[i] * x[i];
-            if (kHeld < kTile && i == 2)
+            if (kHeld < K && i == 2)
 #pragma unroll
                 for (int k = 0; k < S; ++k) half[k] = h[k];
             float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -401,26 +402,26 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
                 if (GATE) y[i] *= z[i] * sigmoid_of(z[i]);
             } else time += l.q < left ? dt[i] : 0.0f;
         };
-        if (steps == kTile) {
+        if (steps == K) {
 #pragma unroll
-            for (int i = 0; i < kTile / 4; ++i) group(i, 4);
+            for (int i = 0; i < K / 4; ++i) group(i, 4);
         } else
 #pragma unroll
-            for (int i = 0; i < kTile / 4; ++i)
+            for (int i = 0; i < K / 4; ++i)
                 if (4 * i < steps) group(i, steps - 4 * i);
-        if (more) take(min(kTile, next.t_end - t_next), buffer ^ 1);
+        if (more) take(min(K, next.t_end - t_next), buffer ^ 1);
         if (Y) {
             const int64_t at = l.at(here.v, t), four = 4 * s.n * s.f;
-            if (steps == kTile) {
+            if (steps == K) {
 #pragma unroll
-                for (int i = 0; i < kTile / 4; ++i) Elem<BF16>::put(static_cast<E *>(s.y) + at + i * four, y[i]);
+                for (int i = 0; i < K / 4; ++i) Elem<BF16>::put(static_cast<E *>(s.y) + at + i * four, y[i]);
             } else
 #pragma unroll
-                for (int i = 0; i < kTile / 4; ++i)
+                for (int i = 0; i < K / 4; ++i)
                     if (4 * i + l.q < steps) Elem<BF16>::put(static_cast<E *>(s.y) + at + i * four, y[i]);
-            if (kHeld < kTile && s.checkpoints && steps > kHeld) store_state(s.checkpoints + l.state(t / kHeld + 1, here.v), half);
+            if (kHeld < K && s.checkpoints && steps > kHeld) store_state(s.checkpoints + l.state(t / kHeld + 1, here.v), half);
         }
-        if (t + kTile >= here.t_end) {    // the sequence ends here, or this piece of it
+        if (t + K >= here.t_end) {    // the sequence ends here, or this piece of it
             if (Y) {
                 for (int o = max(here.t0, here.t_end); o < here.t1; o += 4)
                     if (o + l.q < here.t1) Elem<BF16>::put(static_cast<E *>(s.y) + l.at(here.v, o), 0.0f);
@@ -438,15 +439,15 @@ template <bool BF16, int S, bool Y, bool GATE> __device__ __forceinline__ void s
     }
 }
 
-template <bool BF16, int S, bool GATE> __global__ __launch_bounds__(kWaves *kWave) void scan_kernel(Scan s) {
-    __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
-    scan_tiles<BF16, S, true, GATE>(s, s_rows);
+template <bool BF16, int S, bool GATE, int K> __global__ __launch_bounds__(kWaves *kWave) void scan_kernel(Scan s) {
+    __shared__ float s_rows[kWaves * 2 * K * 8 * S];
+    scan_tiles<BF16, S, K, true, GATE>(s, s_rows);
 }
 // Where there are few sequences the time axis is cut into pieces, and this goes ahead over all but the last one: 3 x 16411 x 128 bf16 in 147
 // pieces takes 31 us here, 7 to join and 40 for the outputs, where one wavefront per sixteen channels would walk 1026 tiles, 2 us each.
 template <bool BF16, int S> __global__ __launch_bounds__(kWaves *kWave) void scan_piece_kernel(Scan s) {
     __shared__ float s_rows[kWaves * 2 * kTile * 8 * S];
-    scan_tiles<BF16, S, false, false>(s, s_rows);
+    scan_tiles<BF16, S, kTile, false, false>(s, s_rows);
 }
 
 // One timestep, the step of a model that follows a running series: a wavefront per sixteen channels of a sequence and no more.  The state
@@ -631,7 +632,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
     }
 }
 
-// Timesteps of a tile of the adjoint: what a wavefront fetches ahead.  Sixteen where the registers hold them (64 sequences of 1024 x 128 bf16: 181 us
+// Timesteps of a tile of the adjoint at most: what a wavefront fetches ahead.  Sixteen where the registers hold them (64 sequences of 1024 x 128 bf16: 181 us
 // against 189 with eight; with 8 states, at three wavefronts per SIMD, 188 with eight and 200 with sixteen; with 32 they spill).
 template <int S> constexpr int kBackTile = S == 4 ? 16 : 8;
 // Whether a tile's loads are all made, whatever is there of it.  With 32 states, where the registers are short, the loads that a branch may
@@ -639,17 +640,15 @@ template <int S> constexpr int kBackTile = S == 4 ? 16 : 8;
 // addresses that take the branches' place do where half of a tile is there (7 x 20000 x 64: 230 against 209; 16 x 8192 x 128: 281 against 278), and with 8 neither.
 template <bool BF16, int S> constexpr bool kAllLoads = S > 4 || (BF16 && S == 4);
 
-template <bool BF16, int S> struct BackTile {
-    static constexpr int K = kBackTile<S>;
+template <bool BF16, int S, int K> struct BackTile {
     Rows<BF16, S, K> rows;
     float x[K / 4], delta[K / 4], gy[K / 4], z[K / 4], h[K / kHeld][S], k[S];
 };
 
 // `k`: what reaches the last tile of a piece from behind.
-template <bool BF16, int S, bool GATE>
-__device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanBack &b, const Lane<S> &l, const Place &p, int t, int steps, bool last) {
+template <bool BF16, int S, int K, bool GATE>
+__device__ __forceinline__ void load_back_tile(BackTile<BF16, S, K> &r, const ScanBack &b, const Lane<S> &l, const Place &p, int t, int steps, bool last) {
     typedef typename Elem<BF16>::Type E;
-    constexpr int K = kBackTile<S>;
     const Scan &s = b.s;
     const int64_t first = l.at(p.v, t), frame = s.n * s.f;
     auto values = [&](int i, int64_t at) {
@@ -686,10 +685,10 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S> &r, const ScanB
 // states, and they are what bounds it: 16 x 50021 x 32 fp32 takes 425 us with vector instructions in 80 % of the cycles at two wavefronts per SIMD, 2.9
 // TB/s with the forward pass.  The exchange over channels is 16 of them, its cost when left out 19 %; the matrix cores would take the sums at the same number of
 // issue slots.  16 x 8192 x 128 fp32: 188 us with 8 states, 279 with 16; 16 x 4096 x 128 with 32: 289, bf16 267.
-template <bool BF16, int S, bool GATE>
+template <bool BF16, int S, bool GATE, int K>
 __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
-    constexpr int N = 4 * S, K = kBackTile<S>, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
+    constexpr int N = 4 * S, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
     constexpr int J = S <= 4 ? 4 : 2;                                     // timesteps whose sums over channels are exchanged together
     // With 32 states in fp32 what two fours have in flight together does not fit the registers: they stay apart (16 x 4096 x 128: 291 us against 334);
     // in bf16 it does (253 against 277).
@@ -723,7 +722,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
     int t = more ? last_tile(here) : 0, buffer = 0;
     // the lane's own timesteps: t + 4 i + q
     float x[R], dt[R], sig[R], gp[R], gz[R], h0[K / kHeld][S], k[S], from_behind[S];
-    BackTile<BF16, S> r;
+    BackTile<BF16, S, K> r;
     auto take = [&](int steps, float *to) {
         r.rows.template stage<kAllLoads<BF16, S>>(to, lane, steps);
 #pragma unroll
@@ -746,7 +745,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
         for (int i = 0; i < S; ++i) from_behind[i] = r.k[i];
     };
     if (more) {
-        load_back_tile<BF16, S, GATE>(r, b, l, here, t, min(K, here.t_end - t), true);
+        load_back_tile<BF16, S, K, GATE>(r, b, l, here, t, min(K, here.t_end - t), true);
         take(min(K, here.t_end - t), s_mem + wave * V);
     }
     while (more) {
@@ -766,7 +765,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
         // The next tile's loads go out now and are taken up behind this one's stores, whose number is known: loads and stores are counted in
         // one order, and waiting for the loads is waiting until no more than the stores are left.
         const int steps_next = min(K, next.t_end - t_next);
-        if (more) load_back_tile<BF16, S, GATE>(r, b, l, next, t_next, steps_next, t_next == last_tile(next));
+        if (more) load_back_tile<BF16, S, K, GATE>(r, b, l, next, t_next, steps_next, t_next == last_tile(next));
         const int64_t at = l.at(here.v, t), four = 4 * s.n * s.f;
         wave_lds_sync();
         float h[S], held[kHeld][S];
@@ -960,6 +959,14 @@ int check_shape(int64_t T, int64_t n, int32_t f, int32_t N) {
     return DGNN_OK;                       // a place behind the last piece still is an int
 }
 
+// Tiles of eight timesteps where the series is short: half the loads that nothing is there for, fewer registers, more wavefronts (fp32, 16 x 100003 x
+// 64 with the state handed on: 650 us against 691; 40 x 3200 x 64 42 against 46; 57 x 1501 x 48 the same; 256 x 256 x 128 53 against 49).  bf16 from
+// twelve timesteps down (8 x 16000 x 64 48 us against 57, 12 x 11000 x 64 51 against 54; 16 x 100003 x 64 591 against 563).
+bool short_ahead(int64_t T, dgnn_dtype dt) { return T <= (dt == DGNN_F32 ? 48 : 12); }
+// The adjoint with 16 states likewise: 8 x 16000 x 64 145 us against 171, bf16 142 against 178; 12 x 11000 x 64 156 against 162, bf16 164 against
+// 157; 16 x 50021 x 32 447 against 413.
+bool short_back(int64_t T) { return T <= 8; }
+
 struct Pieces { int chunk, count; };
 
 // The time axis in pieces of whole tiles where there is less work across it than the device holds: `items` walks side by side (going ahead a wavefront's,
@@ -969,10 +976,10 @@ struct Pieces { int chunk, count; };
 // 11.1), 32 back (48 of two: 20 against 29 us, 32 of a hundred: 24.7 against 22.6).  Twice as many tiles to a piece cost 10 - 20 % at a few hundred
 // timesteps (16 sequences of 128 x 64: 14.5 us for 12.1); no more pieces than one join takes.
 Pieces pieces_of(int64_t T, int64_t items, int64_t wanted, int64_t least, int64_t least_tiles) {
-    const int64_t tiles = (T + kTile - 1) / kTile;
+    const int64_t tiles = (T + kPiece - 1) / kPiece;
     const int64_t count = std::min<int64_t>({tiles, wanted / items, kJoinRuns * kJoin});
-    if (count < least || tiles < least_tiles) return {(int)(tiles * kTile), 1};
-    const int64_t chunk = (tiles + count - 1) / count * kTile;
+    if (count < least || tiles < least_tiles) return {(int)(tiles * kPiece), 1};
+    const int64_t chunk = (tiles + count - 1) / count * kPiece;
     return {(int)chunk, (int)((T + chunk - 1) / chunk)};
 }
 
@@ -1095,8 +1102,13 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
             hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((n * s.groups + kWaves - 1) / kWaves, kMaxGrid)), dim3(kWaves * kWave), 0, st, s);
         });
     return by_kind(dt, states, [&](auto bf16, auto per) {
-        const auto kernel = z ? scan_kernel<decltype(bf16)::value, decltype(per)::value, true> : scan_kernel<decltype(bf16)::value, decltype(per)::value, false>;
-        hipLaunchKernelGGL(kernel, walk_grid(kernel, s, s.pieces), dim3(kWaves * kWave), 0, st, s);
+        auto launch = [&](auto tile) {
+            constexpr int K = decltype(tile)::value;
+            const auto kernel = z ? scan_kernel<decltype(bf16)::value, decltype(per)::value, true, K> : scan_kernel<decltype(bf16)::value, decltype(per)::value, false, K>;
+            hipLaunchKernelGGL(kernel, walk_grid(kernel, s, s.pieces), dim3(kWaves * kWave), 0, st, s);
+        };
+        if (short_ahead(T, dt)) launch(std::integral_constant<int, kHeld>{});
+        else launch(std::integral_constant<int, kTile>{});
     });
 }
 
@@ -1155,9 +1167,14 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
     }
     int rc = by_kind(dt, states, [&](auto bf16, auto per) {
         constexpr int S = decltype(per)::value;
-        const unsigned lds = shape.waves * (3u * kBackTile<S> * 8 * S * sizeof(float) + (S + 2) * kWave * sizeof(double));
-        const auto kernel = z ? scan_back_kernel<decltype(bf16)::value, S, true> : scan_back_kernel<decltype(bf16)::value, S, false>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(shape.slots * shape.blocks_of_groups)), dim3(shape.waves * kWave), lds, st, b);
+        auto launch = [&](auto tile) {
+            constexpr int K = decltype(tile)::value;
+            const unsigned lds = shape.waves * (3u * K * 8 * S * sizeof(float) + (S + 2) * kWave * sizeof(double));
+            const auto kernel = z ? scan_back_kernel<decltype(bf16)::value, S, true, K> : scan_back_kernel<decltype(bf16)::value, S, false, K>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(shape.slots * shape.blocks_of_groups)), dim3(shape.waves * kWave), lds, st, b);
+        };
+        if (short_back(T)) launch(std::integral_constant<int, kHeld>{});
+        else launch(std::integral_constant<int, kBackTile<S>>{});
     });
     if (rc) return rc;
     const int width = f * (states + 2);
