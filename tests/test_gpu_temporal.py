@@ -166,7 +166,8 @@ class Scan:
         if self.lengths is not None:
             gone = torch.arange(self.T)[:, None] >= self.lengths.clamp(0, self.T)[None, :]
             for t in (self.x, self.delta, self.bc, self.z, self.g_y):
-                t[gone] = NAN
+                if t is not None:
+                    t[gone] = NAN
         return self
 
     def inputs(self):
@@ -245,6 +246,16 @@ def test_scan_very_long(N):
 @pytest.mark.parametrize("T", [1, 6, 16, 37, 400])
 def test_scan_lengths(T, N):
     Scan(T, 9, 32, N, F32, seed=N, lengths=[0, 1, T, T - 1, T + 9, -3, T // 2, T // 3, min(T, 17)]).poison().check()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [8, 16, 32])
+@pytest.mark.parametrize("T", [2, 8, 9, 12, 13, 48, 49])
+def test_scan_lengths_around_tiles(T, N, dtype):
+    """Where tiles of eight timesteps give way to those of sixteen, either way and in either type; widths of more than one workgroup too."""
+    lengths = [0, T, 1, 8, T - 1, T // 2, 9]
+    Scan(T, 7, 48, N, dtype, seed=T + N, lengths=lengths).poison().check()
+    Scan(T, 7, 160, N, dtype, seed=T + N, lengths=lengths, z=False).poison().check()
 
 
 @pytest.mark.parametrize("T", [5, 400])
