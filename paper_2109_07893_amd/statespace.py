@@ -6,7 +6,7 @@ input).  With frames x [T, n, f] and an inner width d,
     delta = u W_dt,  bc = u W_bc       dgnn_feature_transform        y = scan(u, delta, bc, z)      dgnn_selective_scan
     out = y W_out                      dgnn_feature_transform
 
-Sequences are vertices; `lengths` says how many timesteps of the block each has.  A series in blocks (Section "Gradient Checkpoint"): the
+Sequences are vertices; `lengths` says how many timesteps of the block each has (frames and gradients behind them may hold anything).  A series in blocks (Section "Gradient Checkpoint"): the
 layer holds the last frames and the state between calls, and backward() takes and leaves their gradients.  Buffers and call order only;
 the arithmetic is in the HIP kernels."""
 from __future__ import annotations
@@ -96,10 +96,20 @@ class StateSpaceLayer(ClipsGradients):
         self.g_y, self.dz, self.du, self.ddelta, self.du0, self.more = (empty(self.y) for _ in range(6))
         self.dbc, self.dx, self.dx_more = empty(self.bc), empty(self.out), empty(self.out)
         self.dframes, self.dstate = empty(self.frames), empty(self.state)
+        self.as_it_is = torch.zeros((2, self.f), device=self.dev)                      # the taps of a convolution that changes nothing
+        self.as_it_is[0] = 1.0
         need = [B.selective_scan_backward_workspace(self.T, self.n, self.d, self.states),
                 B.causal_conv_backward_workspace(self.T, self.n, self.d, self.weights["taps"].shape[0])]
         need += [B.weight_grad_workspace(*self.weights[k].shape) for k in WEIGHTS]
         self.ws_back = torch.empty(max(need), dtype=torch.uint8, device=self.dev)
+
+    def _there(self, t: torch.Tensor) -> torch.Tensor:
+        """Frames [T, n, f] with zeros behind the sequences' ends, in dx_more: a weight gradient sums over all rows, where what lies there (anything)
+        meets zeros, and zero times NaN or infinity is NaN."""
+        if self.lengths is None:
+            return t
+        B.causal_conv(t.contiguous(), self.as_it_is, None, self.dx_more, lengths=self.lengths)
+        return self.dx_more
 
     def backward(self, g_out: torch.Tensor, behind=None, accumulate: bool = False) -> torch.Tensor:
         """g_out [T, n, f] = dL/d(output frames) of the last forward(), which was one with train; returns dL/dx [T, n, f].  behind = (gradient of the frames,
@@ -115,7 +125,7 @@ class StateSpaceLayer(ClipsGradients):
         dframes, dstate = behind or (None, None)
         p, g, ws, flat = self.weights, self.grads, self.ws_back, lambda t: t.reshape(-1, t.shape[-1])  # noqa: E731
         wgrad = lambda x, gy, name: B.weight_grad(flat(x), flat(gy), g[name], ws, accumulate=accumulate)  # noqa: E731
-        wgrad(self.y, g_out, "w_out")
+        wgrad(self.y, self._there(g_out), "w_out")
         B.input_grad(flat(g_out), p["w_out"], flat(self.g_y))
         B.selective_scan_backward(self.u, self.delta, self.bc, p["a"], self.g_y, self.checkpoints, self.du, self.ddelta, self.dbc, g["a"], ws, z=self.z, dz=self.dz,
                                   d=p["d"], dd=g["d"], dt_bias=p["dt_bias"], ddt_bias=g["dt_bias"], dh_after=dstate, dh_before=self.dstate, lengths=self.lengths,
@@ -126,8 +136,9 @@ class StateSpaceLayer(ClipsGradients):
             B.add(flat(self.du), flat(self.more), flat(self.du))
         B.causal_conv_backward(self.u0, p["taps"], p["conv_bias"], self.du, self.du0, g["taps"], g["conv_bias"], ws, silu=True, x_before=self.frames_before,
                                dx_after=dframes, dx_before=self.dframes, lengths=self.lengths, accumulate=accumulate)
-        wgrad(self.x, self.du0, "w_in")
-        wgrad(self.x, self.dz, "w_z")
+        x = self._there(self.x)
+        wgrad(x, self.du0, "w_in")
+        wgrad(x, self.dz, "w_z")
         B.input_grad(flat(self.du0), p["w_in"], flat(self.dx))
         B.input_grad(flat(self.dz), p["w_z"], flat(self.dx_more))
         B.add(flat(self.dx), flat(self.dx_more), flat(self.dx))

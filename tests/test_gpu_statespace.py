@@ -261,3 +261,42 @@ def test_refusals():
         layer.forward(torch.zeros((2, 4, 16), device=DEV))
     with pytest.raises(ValueError):
         layer.step(torch.zeros((4, 16), device=DEV, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,n,f,d,states,w", [(1, 33, 16, 32, 8, 4), (40, 7, 64, 128, 32, 3), (5, 300, 16, 16, 8, 2)])
+def test_layer_padding_may_hold_anything(T, n, f, d, states, w, dtype):
+    """NaN and infinities in frames and gradients behind a sequence's end: bit for bit what zeros there give, in fp32 near 64 bits too."""
+    p = make_weights(f, d, states, w, dtype=dtype)
+    g = torch.Generator().manual_seed(8)
+    lengths = torch.randint(0, T + 1, (n,), generator=g, dtype=torch.int32)
+    lengths[:2] = torch.tensor([0, T])
+    gone = torch.arange(T)[:, None] >= lengths[None, :]
+    x, g_out = torch.randn((T, n, f), generator=g).to(dtype), torch.randn((T, n, f), generator=g).to(dtype)
+
+    def passes(fill):
+        frames, grad = x.clone(), g_out.clone()
+        frames[gone], grad[gone] = torch.tensor(fill, dtype=dtype), torch.tensor(fill, dtype=dtype)
+        layer = StateSpaceLayer(n, T, p, lengths=lengths.to(DEV))
+        frames, grad = frames.to(DEV), grad.to(DEV)
+        res = [layer.forward(frames, train=True).clone(), layer.backward(grad).clone()]
+        grads = {k: v.clone() for k, v in layer.grads.items()}
+        layer.backward(grad, accumulate=True)
+        assert all(torch.allclose(layer.grads[k], 2 * v, rtol=1e-5, atol=1e-6 * float(v.abs().max())) for k, v in grads.items())
+        assert torch.equal(frames[gone.to(DEV)].isnan(), torch.full_like(frames[gone.to(DEV)], fill).isnan())          # inputs stay as they are
+        return res, grads
+
+    (out, dx), grads = passes(0.0)
+    for fill in (float("nan"), float("inf"), -float("inf")):
+        (out_p, dx_p), grads_p = passes(fill)
+        assert torch.equal(out, out_p) and torch.equal(dx, dx_p), fill
+        for k in WEIGHTS + PARAMETERS:
+            assert torch.equal(grads[k], grads_p[k]), (fill, k)
+    assert not out[gone.to(DEV)].any() and not dx[gone.to(DEV)].any()
+    if dtype == torch.float32:
+        x[gone], g_out[gone] = 0.0, 0.0
+        want, want_dx, want_grads = oracle_layer(p, x, g_out, lengths.numpy())
+        near(out, want, "out")
+        near(dx, want_dx, "dx")
+        for k in WEIGHTS + PARAMETERS:
+            near(grads[k], want_grads[k], k)
