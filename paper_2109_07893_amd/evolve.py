@@ -38,7 +38,10 @@ class EvolvingWeights(ClipsGradients):
         return list(self.frames)
 
     def backward(self, dw_t: List[torch.Tensor]) -> None:
-        """dw_t[t-1] = dL/dW_t (fp32, from the GCN steps).  Leaves dL/dU_x, dL/dU_h, dL/db and dL/dW_0."""
+        """dw_t[t-1] = dL/dW_t (fp32, from the GCN steps, as they leave them).  Leaves dL/dU_x, dL/dU_h, dL/db and dL/dW_0: these are what
+        clip_gradients() belongs to; a trainer's would scale them by the norm over dL/dW_t, and is refused here."""
+        if any(getattr(g, "clipped", False) for g in dw_t):
+            raise ValueError("the trainer's clip_gradients() has scaled dL/dW_t: clip the gradients that come out of EvolvingWeights.backward() instead")
         B.evolve_weights_backward(self.w0, self.u_x, self.u_h, self.bias, self.w, self.c, dw_t, self.dw0, self.du_x, self.du_h, self.db, self.ws)
 
     def parameter_gradients(self) -> List[torch.Tensor]:

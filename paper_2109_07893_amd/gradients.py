@@ -70,3 +70,28 @@ class ClipsGradients:
         else:
             bound.bind()
         return bound.clip(max_norm)
+
+
+class ClipsBlockGradients(ClipsGradients):
+    """The same for a trainer over a block: `dw`, or dw_t[timestep][layer] where every timestep has weights of its own.  Those are either
+    parameters themselves, or come out of EvolvingWeights, whose backward() forms the parameters' gradients from dw_t: then it is its
+    gradients that are clipped, afterwards, and it refuses a dw_t that was scaled ahead of it."""
+
+    _timesteps_clipped = False
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return self.dw if self.dw_t is None else [g for t in range(self.blk.T) for g in self.dw_t[t]]
+
+    def clip_gradients(self, max_norm: float) -> torch.Tensor:
+        norm = super().clip_gradients(max_norm)
+        if self.dw_t is not None:
+            self._mark_timesteps(True)
+        return norm
+
+    def _mark_timesteps(self, clipped: bool) -> None:
+        """backward() takes the mark off again."""
+        if clipped or self._timesteps_clipped:
+            for layers in self.dw_t:
+                for g in layers:
+                    g.clipped = clipped
+        self._timesteps_clipped = clipped

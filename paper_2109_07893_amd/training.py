@@ -33,7 +33,7 @@ import torch
 
 from . import binding as B
 from .batch import GATHERED_DINV_ROWS, SERIES_ENTRIES, Frames, SeriesTable, SmoothTable, SpmmTable, TransformTable, WeightGradTable, pointers, series_pays, snapshots_fit, steps_together, upstream_frames
-from .gradients import ClipsGradients
+from .gradients import ClipsBlockGradients, ClipsGradients
 from .pipeline import BlockInputs, BlockRunner
 
 
@@ -256,7 +256,7 @@ class GcnStack:
             g = dst
 
 
-class BlockTrainer(ClipsGradients):
+class BlockTrainer(ClipsBlockGradients):
     """Forward and backward over one block; gradients of the layer weights (fp32) come out in `dw`."""
 
     def __init__(self, blk: BlockInputs, directed: bool,
@@ -406,6 +406,7 @@ class BlockTrainer(ClipsGradients):
         else:
             g_top = g_y
         self.g_top = None if masked else g_top
+        self._mark_timesteps(False)
         m = stack.steps_back(self.dw_t, T)
         last = (T - 1) // m * m
         for t in range(last, -1, -m):
@@ -416,10 +417,6 @@ class BlockTrainer(ClipsGradients):
             if stack.needs_transposed and t >= 2 and not self.keep_snapshots:   # A_{t-1} from A_t: the lists exchanged (A_1 was kept)
                 for chain, lists, _ in self._chains():
                     self._rebuild(chain, lists[t - 1], blk.nnz[t], t + 1, t, reverse=True)
-
-
-    def parameter_gradients(self) -> List[torch.Tensor]:
-        return self.dw if self.dw_t is None else [g for t in range(self.blk.T) for g in self.dw_t[t]]
 
     @property
     def h(self) -> torch.Tensor:
@@ -618,7 +615,7 @@ class _Ring:
         return self.rowptr[s], self.colidx[s], nnz
 
 
-class SmoothedTrainer(ClipsGradients):
+class SmoothedTrainer(ClipsBlockGradients):
     """A training step on SMOOTHED snapshots (Section "Smoothening the Input Graphs": the graphs TM-GCN and EvolveGCN
     are trained on), with the smoothing done on the device: every S_t and its normalisation by dgnn_smooth_series, or, for
     series longer than one such call takes, the raw A_t by dgnn_delta_rebuild, S_t = S_{t-1} + A_t - A_{t-life} by
@@ -734,9 +731,6 @@ class SmoothedTrainer(ClipsGradients):
             with self._stage("csr_weighted_dinv"):
                 B.csr_weighted_dinv(rp, val, self.s_nnz[t - 1], self.dinv_s[t - 1], self.ws_dinv)
 
-    def parameter_gradients(self) -> List[torch.Tensor]:
-        return self.dw if self.dw_t is None else [g for t in range(self.blk.T) for g in self.dw_t[t]]
-
     def forward(self) -> torch.Tensor:
         blk, stack = self.blk, self.stack
         stream = torch.cuda.current_stream(self.dev).cuda_stream
@@ -772,6 +766,7 @@ class SmoothedTrainer(ClipsGradients):
             g_top = self.g
         else:
             g_top = g_y
+        self._mark_timesteps(False)
         m = stack.steps_back(self.dw_t, T)
         last = (T - 1) // m * m
         for t in range(last, -1, -m):

@@ -300,3 +300,29 @@ def test_layer_padding_may_hold_anything(T, n, f, d, states, w, dtype):
         near(dx, want_dx, "dx")
         for k in WEIGHTS + PARAMETERS:
             near(grads[k], want_grads[k], k)
+
+
+@pytest.mark.parametrize("smoothed", [False, True])
+def test_evolving_weights_take_gradients_before_they_are_clipped(smoothed):
+    """dL/dW_t are what the evolution's own gradients are formed from: once a trainer's clip_gradients has scaled them, they are
+    refused until the next pass forms them anew; behind the evolution's backward pass they may be clipped."""
+    wl = WORKLOADS["c1"]
+    blk = make_block(wl, DEV, gen_device="cpu")
+    g_y = torch.randn((wl.T, wl.n, wl.f), generator=torch.Generator().manual_seed(1)).to(DEV)
+    f = wl.f
+    r = lambda *s: 0.3 * torch.randn(s, generator=torch.Generator().manual_seed(len(s))).to(DEV)  # noqa: E731
+    ev = EvolvingWeights(r(f, f), r(f, 4 * f), r(f, 4 * f), r(4 * f).view(-1), wl.T)
+    blk.w_t = [[w] for w in ev.forward()]
+    tr = make_smoothed_trainer(wl, blk, 3) if smoothed else make_trainer(wl, blk)
+    tr.forward()
+    tr.backward(g_y)
+    ev.backward([g[0] for g in tr.dw_t])
+    want = [g.clone() for g in ev.parameter_gradients()]
+    check_clip(tr, 0.01)
+    with pytest.raises(ValueError, match="clip"):
+        ev.backward([g[0] for g in tr.dw_t])
+    assert all(torch.equal(a, b) for a, b in zip(want, ev.parameter_gradients()))
+    tr.forward()
+    tr.backward(g_y)
+    ev.backward([g[0] for g in tr.dw_t])
+    assert all(torch.equal(a, b) for a, b in zip(want, ev.parameter_gradients()))
