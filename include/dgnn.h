@@ -768,7 +768,8 @@ typedef struct {
 } dgnn_grad_item;
 
 /*
- * norm[0] (DEVICE fp32) = sqrt(sum of g^2 over all items);  dgnn_grad_clip: out = g * min(1, max_norm / (norm + 1e-6)), rounded once.
+ * norm[0] (DEVICE fp32) = sqrt(sum of g^2 over all items);  dgnn_grad_clip: out = g * min(1, max_norm / (norm + 1e-6)): the factor rounded
+ * to fp32 (taken in 64 bits where it is below 2^-126), its product with g to dt.
  * A norm that is no finite number (in fp32) leaves the gradients as they are (out = g): the caller finds it in norm[0].  Squares and sums are
  * in 64 bits, in a fixed order.  What is written overlaps nothing else, but out may be exactly its own g.  items: HOST array, read before
  * the call returns (dgnn_grad_norm does not look at out).  ws: dgnn_grad_clip_workspace(count) bytes, 16-byte aligned.

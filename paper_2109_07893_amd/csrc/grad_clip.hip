@@ -127,12 +127,13 @@ __device__ __forceinline__ double total_of(const double *__restrict__ sums, int 
     return sqrt(block_sum(sum, s_sum));
 }
 
-template <bool BF16> __device__ __forceinline__ void scaled(const uintx4 (&r)[kPer], const Tensors &t, const Stretch &s, float factor) {
+// F: the type of the factor and of its product with a gradient.
+template <bool BF16, typename F> __device__ __forceinline__ void scaled(const uintx4 (&r)[kPer], const Tensors &t, const Stretch &s, F factor) {
     constexpr int NV = Pack<BF16>::kVals;
     typedef typename Elem<BF16>::Type E;
     const E *g = begin_of<BF16>(t, s);
     E *out = as_global(static_cast<E *>(t.out[s.k])) + s.from;
-    auto one = [&](int i) { out[i] = Elem<BF16>::put(Elem<BF16>::get(g[i]) * factor); };
+    auto one = [&](int i) { out[i] = Elem<BF16>::put((float)((F)Elem<BF16>::get(g[i]) * factor)); };
     if ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) {       // no boundary in common
         for (int i = threadIdx.x; i < s.count; i += kThreads) one(i);
         return;
@@ -145,7 +146,7 @@ template <bool BF16> __device__ __forceinline__ void scaled(const uintx4 (&r)[kP
         float v[NV];
         Pack<BF16>::unpack(v, r[u]);
 #pragma unroll
-        for (int e = 0; e < NV; ++e) v[e] *= factor;
+        for (int e = 0; e < NV; ++e) v[e] = (float)((F)v[e] * factor);
         if ((int)threadIdx.x + u * kThreads < s.pieces) o[u * kThreads] = Pack<BF16>::pack(v);
     }
 }
@@ -167,8 +168,12 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Tensors t, const d
     const double most = max_norm / (total + 1e-6);
     const bool clip = isfinite((float)total) && most < 1.0;  // a norm that *norm shows as no finite number: nothing to scale by
     const float factor = clip ? (float)most : 1.0f;
+    // A factor below the normal numbers of 32 bits keeps few of its digits there, or none, where its product with a large gradient has all of them.
+    const bool small = clip && most < 0x1p-126;
     while (i >= 0) {
-        if (clip || t.out[s.k] != t.g[s.k]) {
+        if (small) {
+            if (t.bf16[s.k]) scaled<true>(r, t, s, most); else scaled<false>(r, t, s, most);
+        } else if (clip || t.out[s.k] != t.g[s.k]) {
             if (t.bf16[s.k]) scaled<true>(r, t, s, factor); else scaled<false>(r, t, s, factor);
         }
         i -= gridDim.x;

@@ -144,3 +144,22 @@ def test_repeats_and_graph():
         torch.cuda.synchronize()
         assert torch.equal(set_.scalar, norm) and all(torch.equal(a, b) for a, b in zip(out, eager))
         dg.Gradients(grads[:5]).norm()
+
+
+@pytest.mark.parametrize("max_norm", [1.0, 0.01, 1e-8, 1e-25, 1e-44])
+@pytest.mark.parametrize("scale", [1e30, 2.7e37])
+def test_factor_below_float(scale, max_norm):
+    """max_norm / norm that 32 bits hold with few digits or not at all: its product with a gradient is still a number of theirs.  Either the
+    factor and the product are rounded, 2^-24 each, or the product alone; bf16 rounds once more; and half of the smallest fp32 number
+    (and of bf16's, 2^-134) where results are below the normal range."""
+    grads = make([((77,), F32), ((5, 3), BF16), ((9,), F32)], scale=scale, seed=4)
+    before, norm = [g.clone() for g in grads], norm_of(grads)
+    assert norm < 3.4e38
+    out = [torch.full_like(g, float("nan")) for g in grads]
+    dg.Gradients(grads, out).clip(max_norm)
+    assert abs(float(dg.Gradients(grads).clip(max_norm)) - norm) <= norm * (2.0 ** -24 + 2.0 ** -40)
+    factor = max_norm / (norm + 1e-6)
+    for a, b, c in zip(before, grads, out):
+        want, tiny = a.double() * factor, 2.0 ** -150 if a.dtype == F32 else 2.0 ** -134 + 2.0 ** -150
+        bound = want.abs() * (torch.finfo(a.dtype).eps / 2 + 2 * 2.0 ** -24) * (1 + 2.0 ** -10) + tiny
+        assert torch.equal(b, c) and bool(((b.double() - want).abs() <= bound).all())
