@@ -722,7 +722,8 @@ int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bia
  *   x, delta, y [T][n][f]        storage type dt
  *   bc [T][n][2 N]               B | C of a sequence's timestep, which its channels share: one product of dgnn_feature_transform
  *   z [T][n][f]                  or NULL (no gate)
- *   a [f][N]; d [f], dt_bias [f] or NULL (zero)
+ *   a [f][N]; d [f], dt_bias [f] or NULL (zero).  An a of minus infinity forgets what a timestep of a
+ *                                step size of 1e-36 or more finds
  *   h_before [n][f][N] fp32      the state ahead of the series, or NULL (zero)
  *   h_after [n][f][N] fp32       receives the last state, or NULL; may be h_before
  *   checkpoints                  NULL, or fp32 of dgnn_selective_scan_checkpoints() bytes: the state ahead of every 8th timestep,

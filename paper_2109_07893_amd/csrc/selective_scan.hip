@@ -216,6 +216,13 @@ template <int S> __device__ __forceinline__ void load_decay(float (&a2)[S], cons
 #pragma unroll
     for (int s = 0; s < S; ++s) a2[s] *= kLog2e;
 }
+// The same going back, the largest number of its sign where that is infinite: a state that is forgotten at once (a of minus infinity) has a decay of
+// zero, which meets a2 there, and timesteps that are not there have a step size of zero; zero times infinity is NaN.
+template <int S> __device__ __forceinline__ void load_decay_back(float (&a2)[S], const float *a, int ch, int q) {
+    load_decay(a2, a, ch, q);
+#pragma unroll
+    for (int s = 0; s < S; ++s) a2[s] = fabsf(a2[s]) == __builtin_inff() ? copysignf(3.402823466e38f, a2[s]) : a2[s];
+}
 
 // Sequence v in piece p of the time axis: timesteps [t0, t1), of which the sequence has those ahead of t_end.
 struct Place {
@@ -573,7 +580,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
     const Lane<S> l(s, w % s.groups, lane);
     const float bias = s.dt_bias ? s.dt_bias[l.ch] : 0.0f;
     float a2[S];
-    load_decay(a2, s.a, l.ch, l.q);
+    load_decay_back(a2, s.a, l.ch, l.q);
     for (Place here{w / s.groups, 1, 0, 0, 0}; here.settle(s, s.pieces); here.v += stride) {
         Rows<BF16, S, kTile> bc;
         float k[S], time = 0.0f, delta[R], gy[R], z[R];
@@ -705,7 +712,7 @@ __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(Sc
     const Lane<S> l(s, g, lane);
     const int q = l.q, turn = waves * V;
     float a2[S], acc[S + 2];                                              // sums over a few tiles: da of the lane's states, dd, ddt_bias
-    load_decay(a2, s.a, l.ch, q);
+    load_decay_back(a2, s.a, l.ch, q);
     double *const sums = reinterpret_cast<double *>(s_mem + 3 * turn) + wave * (S + 2) * kWave + lane;
 #pragma unroll
     for (int i = 0; i < S + 2; ++i) { sums[i * kWave] = 0.0; acc[i] = 0.0f; }

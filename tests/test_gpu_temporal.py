@@ -508,3 +508,40 @@ def test_two_streams_and_two_graphs():
         for graph in graphs:
             graph.replay()
         check()
+
+
+class Forgetful(Scan):
+    """Every second state with a of minus infinity, which 64 bits are given as -1e30: exp(-1e30 dt) = 0 there for every step size met."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        self.a[:, ::2] = -float("inf")
+
+    def oracle(self):
+        a = super().oracle()
+        return dict(a, a=np.where(np.isinf(a["a"]), -1e30, a["a"]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [8, 16, 32])
+@pytest.mark.parametrize("T,n,f", [(1, 7, 32), (5, 7, 32), (13, 7, 48), (50, 7, 160), (400, 3, 16)])
+def test_scan_no_state_kept_going_back(T, n, f, N, dtype):
+    """... and its gradients: what a timestep finds has none, a sequence without a timestep hands its gradient on as it is."""
+    lengths = [0, T, 1, T - 1, T // 2, 2, T][:n]
+    s = Forgetful(T, n, f, N, dtype, seed=T + N, lengths=lengths).poison()
+    s.check()
+    got = s.backward(s.forward()[2])
+    assert torch.equal(got["dh_before"][0].cpu(), s.dh_after[0])
+
+
+def test_scan_all_states_forgotten():
+    """No sequence of different lengths, and growth without bound where no timestep follows."""
+    s = Forgetful(21, 4, 32, 16, F32)
+    s.a[:] = -float("inf")
+    s.check()
+    s = Scan(21, 4, 32, 16, F32, lengths=[0, 0, 0, 0])
+    s.a[:] = float("inf")
+    y, after, kept = s.forward()
+    got = s.backward(kept)
+    assert not y.any() and torch.equal(after.cpu(), s.h_before) and torch.equal(got["dh_before"].cpu(), s.dh_after)
+    assert not any(got[k].any() for k in got if k != "dh_before")
