@@ -85,10 +85,12 @@ class StateSpaceLayer(ClipsGradients):
             self.x = x
         return self._run(x, (self.u0, self.u, self.z, self.delta, self.y, self.bc, self.out), self.lengths, self.checkpoints if train else None)
 
-    def step(self, x: torch.Tensor) -> torch.Tensor:
-        """One timestep further: frames [n, f] in and out (a buffer of the layer's, which the next step may take in)."""
+    def step(self, x: torch.Tensor, lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One timestep further: frames [n, f] in and out (a buffer of the layer's, which the next step may take in).  lengths [n] int32, 1 or 0: a
+        sequence of 0 keeps its frames and its state, its output is zero.  Without them every sequence moves on, those too that ended inside
+        of the block."""
         self._check(x, (self.n, self.f))
-        return self._run(x[None], self.one, None, None)[0]
+        return self._run(x[None], self.one, lengths, None)[0]
 
     def _training_buffers(self) -> None:
         empty = lambda like: torch.empty_like(like)  # noqa: E731

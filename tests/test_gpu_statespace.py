@@ -326,3 +326,33 @@ def test_evolving_weights_take_gradients_before_they_are_clipped(smoothed):
     tr.backward(g_y)
     ev.backward([g[0] for g in tr.dw_t])
     assert all(torch.equal(a, b) for a, b in zip(want, ev.parameter_gradients()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_step_of_some_sequences(dtype):
+    """A block of different lengths, then single timesteps of the sequences that go on: the others keep frames and state, whatever their frame
+    holds; without lengths all move on."""
+    T, n, f = 6, 9, 16
+    p = make_weights(f, 32, 8, 4, dtype=dtype)
+    g = torch.Generator().manual_seed(7)
+    x = torch.randn((T + 2, n, f), generator=g).to(DEV).to(dtype)
+    on = torch.tensor([1, 0, 1, 1, 0, 0, 1, 1, 0], dtype=torch.int32, device=DEV)
+    moves = on.bool()
+    layer = StateSpaceLayer(n, T, p, lengths=torch.where(moves, T, torch.arange(n, device=DEV) % T).int())
+    layer.forward(x[:T].contiguous())
+    frames, state = layer.frames.clone(), layer.state.clone()
+    every = StateSpaceLayer(n, T, p)
+    every.frames.copy_(frames)
+    every.state.copy_(state)
+    for t in range(T, T + 2):
+        frame = x[t].clone()
+        frame[~moves] = float("nan")
+        out, want = layer.step(frame, lengths=on), every.step(x[t])
+        assert torch.equal(out[moves], want[moves]) and not out[~moves].any()
+    assert torch.equal(layer.frames[:, moves], every.frames[:, moves]) and torch.equal(layer.state[moves], every.state[moves])
+    assert torch.equal(layer.frames[:, ~moves], frames[:, ~moves]) and torch.equal(layer.state[~moves], state[~moves])
+    assert not torch.equal(every.state[~moves], state[~moves])
+    with pytest.raises(ValueError):
+        layer.step(x[0], lengths=on[:4])
+    with pytest.raises(TypeError):
+        layer.step(x[0], lengths=on.long())
