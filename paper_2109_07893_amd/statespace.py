@@ -82,8 +82,10 @@ class StateSpaceLayer(ClipsGradients):
             if self.checkpoints is None:
                 self.checkpoints = torch.empty(B.selective_scan_checkpoints(self.T, self.n, self.d, self.states), device=self.dev)
             self.frames_before.copy_(self.frames)
-            self.x = x
-        return self._run(x, (self.u0, self.u, self.z, self.delta, self.y, self.bc, self.out), self.lengths, self.checkpoints if train else None)
+        out = self._run(x, (self.u0, self.u, self.z, self.delta, self.y, self.bc, self.out), self.lengths, self.checkpoints if train else None)
+        if train:
+            self.x = x                                                                 # not ahead of a call that is refused half way
+        return out
 
     def step(self, x: torch.Tensor, lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One timestep further: frames [n, f] in and out (a buffer of the layer's, which the next step may take in).  lengths [n] int32, 1 or 0: a

@@ -356,3 +356,18 @@ def test_step_of_some_sequences(dtype):
         layer.step(x[0], lengths=on[:4])
     with pytest.raises(TypeError):
         layer.step(x[0], lengths=on.long())
+
+
+def test_a_refused_forward_leaves_nothing_to_go_back_through():
+    """A forward() that was refused half way has overwritten activations: backward() does not take them for the call before."""
+    p = make_weights(16, 32, 8, 4)
+    layer, x = StateSpaceLayer(4, 3, p), torch.zeros((3, 4, 16), device=DEV)
+    layer.forward(x, train=True)
+    layer.lengths = torch.zeros(5, dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError):
+        layer.forward(x + 1, train=True)
+    layer.lengths = None
+    with pytest.raises(ValueError):
+        layer.backward(x)
+    layer.forward(x, train=True)
+    layer.backward(x)
