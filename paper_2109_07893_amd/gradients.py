@@ -7,13 +7,14 @@ from typing import List, Optional, Sequence
 import torch
 
 from . import binding as B
-from .batch import Table
+from .batch import Table, _data_ptr, _is_contiguous, _numel
 
 
 class Gradients:
     """Gradient tensors (float32 or bfloat16, contiguous, any shapes, on one GPU) that are looked at together, where they lie: the table
-    holds their addresses, so they are bound once and refilled by every step.  `out`: tensors of the same shapes and types that receive
-    the clipped gradients (left out: the gradients themselves)."""
+    holds their addresses and sizes, so they are bound once and refilled by every step; a tensor that was given other memory since is bound()
+    anew ahead of the next call.  `out`: tensors of the same shapes and types that receive the clipped gradients (left out: the gradients
+    themselves)."""
 
     G, OUT, COUNT, DT = range(4)                     # dgnn_grad_item
 
@@ -27,18 +28,27 @@ class Gradients:
         for g, o in zip(self.grads, self.out):
             if o.shape != g.shape or o.dtype != g.dtype or g.device != dev or o.device != dev:
                 raise ValueError("shape, dtype or device mismatch in Gradients")
+        self.in_place = all(o is g for o, g in zip(self.out, self.grads))
+        self.counts, self.index = list(map(_numel, self.grads)), self.grads[0].get_device()
         self.table = Table(len(self.grads), 4)
         self.bind()
-        self.table.column(self.COUNT, [g.numel() for g in self.grads])
+        self.table.column(self.COUNT, self.counts)
         self.table.column(self.DT, [B._dtype_code(g) for g in self.grads])
         self.result = torch.zeros(1, dtype=torch.float32, device=dev)
         self.scalar = self.result[0]
         self.ws = torch.empty(B.grad_clip_workspace(len(self.grads)), dtype=torch.uint8, device=dev)
 
     def bind(self) -> None:
-        """The addresses as they are now (after a tensor was given other memory, which is rare)."""
-        self.table.column(self.G, [B._ptr(g) or 0 for g in self.grads])
-        self.table.column(self.OUT, [B._ptr(o) or 0 for o in self.out])
+        """The addresses as they are now, after a tensor was given other memory (which is rare) of the same size."""
+        self.table.column(self.G, self._addresses(self.grads))
+        self.table.column(self.OUT, self.table.words[:, self.G] if self.in_place else self._addresses(self.out))
+
+    def _addresses(self, tensors: List[torch.Tensor]) -> List[int]:
+        if list(map(_numel, tensors)) != self.counts or any(t.get_device() != self.index for t in tensors):
+            raise ValueError("a tensor of Gradients has another size or device than it was bound with")
+        if not all(map(_is_contiguous, tensors)):
+            raise AssertionError("dgnn takes contiguous tensors")
+        return list(map(_data_ptr, tensors))
 
     def norm(self) -> torch.Tensor:
         """sqrt(sum g^2) over all of them: a scalar on the device, overwritten by the next call."""
@@ -68,7 +78,10 @@ class ClipsGradients:
         if bound is None or len(bound.grads) != len(grads) or any(a is not b for a, b in zip(bound.grads, grads)):
             bound = self._clipped = Gradients(grads)
         else:
-            bound.bind()
+            try:
+                bound.bind()
+            except ValueError:                       # a gradient of another size
+                bound = self._clipped = Gradients(grads)
         return bound.clip(max_norm)
 
 

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2109_07893_amd as dg
+from paper_2109_07893_amd import gradients
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -163,3 +164,32 @@ def test_factor_below_float(scale, max_norm):
         want, tiny = a.double() * factor, 2.0 ** -150 if a.dtype == F32 else 2.0 ** -134 + 2.0 ** -150
         bound = want.abs() * (torch.finfo(a.dtype).eps / 2 + 2 * 2.0 ** -24) * (1 + 2.0 ** -10) + tiny
         assert torch.equal(b, c) and bool(((b.double() - want).abs() <= bound).all())
+
+
+def test_a_tensor_of_another_size_is_refused():
+    """The table holds counts: a gradient that was given memory of another size, or its output, is found where addresses are taken anew."""
+    for of_out in (False, True):
+        grads, out = make([((64,), F32), ((10,), BF16)]), make([((64,), F32), ((10,), BF16)])
+        set_ = dg.Gradients(grads, out)
+        changed = (out if of_out else grads)[0]
+        changed.data = torch.ones(32, device=DEV)
+        with pytest.raises(ValueError):
+            set_.bind()
+        changed.data = torch.ones(8, 8, device=DEV).t()
+        with pytest.raises((ValueError, AssertionError)):
+            set_.bind()
+        changed.data = torch.full((64,), 2.0, device=DEV)
+        set_.bind()
+        assert abs(float(set_.norm()) - norm_of(grads)) <= norm_of(grads) * (2.0 ** -24 + 2.0 ** -40)
+
+    class Trainer(gradients.ClipsGradients):
+        def parameter_gradients(self):
+            return self.grads
+
+    tr = Trainer()
+    tr.grads = make([((64,), F32), ((10,), BF16)])
+    tr.clip_gradients(0.5)
+    tr.grads[0].data = torch.ones(16, device=DEV)                  # other memory, another size: bound anew, not looked at as it was
+    norm = norm_of(tr.grads)
+    assert abs(float(tr.clip_gradients(0.5)) - norm) <= norm * (2.0 ** -24 + 2.0 ** -40)
+    assert norm_of(tr.grads) <= 0.5 * (1 + 2.0 ** -7)
