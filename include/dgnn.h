@@ -697,7 +697,7 @@ int dgnn_add(const void *a, const void *b, void *out, int64_t n, int32_t f, dgnn
  *   x_before [w-1][n][f]   the frames ahead of the series, oldest first, or NULL (zeros)
  *   x_after [w-1][n][f]    receives the last w-1 frames of (x_before, x), or NULL; may be x_before, and no other input or output
  *   flags                  DGNN_SILU or 0
- * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS.
+ * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS (parameters and lengths are inputs too).
  */
 int dgnn_causal_conv(const void *x, const float *taps, const float *bias, const void *x_before, void *y, void *x_after,
                      const int32_t *lengths, int64_t T, int64_t n, int32_t f, int32_t w, uint32_t flags, dgnn_dtype dt, void *stream);
@@ -731,7 +731,7 @@ int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bia
  *   ws                           dgnn_selective_scan_workspace() bytes, 16-byte aligned
  * States, step sizes and sums are fp32, y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose
  * states are joined afterwards: the same sums in another order.  Results repeat bit for bit.
- * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS, CAPACITY.
+ * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS (as above; the workspace is an output), CAPACITY.
  */
 int dgnn_selective_scan_workspace(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);
 int dgnn_selective_scan_checkpoints(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes);

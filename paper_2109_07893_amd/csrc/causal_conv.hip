@@ -326,6 +326,13 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return p && q && p < q + nb && q < p + na;
 }
 
+// Parameters, their gradients and lengths: 32-bit numbers at any address that those may have.
+bool words_aligned(std::initializer_list<const void *> words) {
+    for (const void *p : words)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
+}
+
 // Lanes with work before the time axis stays whole, half of what the device holds at once: pieces read frames twice (64 x 16384 x 64 fp32 going
 // back: 156 us whole, 179 in four pieces), fewer lanes leave loads unissued (128 x 8192 x 64 bf16 going back: 86 us with 2^18 lanes, 118 with 2^17).
 constexpr int64_t kWanted = 1 << 18;
@@ -339,7 +346,12 @@ extern "C" int dgnn_causal_conv(const void *x, const float *taps, const float *b
     if ((dt != DGNN_F32 && dt != DGNN_BF16) || (flags & ~DGNN_SILU)) return DGNN_ERR_SHAPE;
     for (const void *p : {x, x_before, (const void *)y, (const void *)x_after})
         if (p && !aligned16(p)) return DGNN_ERR_ALIGN;
+    if (!words_aligned({taps, bias, lengths})) return DGNN_ERR_ALIGN;
     const size_t row = (size_t)n * f * (dt == DGNN_F32 ? 4 : 2), all = row * T, edge = row * (w - 1);
+    for (auto o : {std::pair<const void *, size_t>{y, all}, {x_after, edge}})
+        if (overlap(o.first, o.second, taps, sizeof(float) * w * f) || overlap(o.first, o.second, bias, sizeof(float) * f) ||
+            overlap(o.first, o.second, lengths, sizeof(int32_t) * n))
+            return DGNN_ERR_ALIAS;
     if (overlap(y, all, x, all) || overlap(y, all, x_before, edge) || overlap(y, all, x_after, edge) || overlap(x_after, edge, x, all) ||
         (x_after != x_before && overlap(x_after, edge, x_before, edge)))
         return DGNN_ERR_ALIAS;
@@ -382,15 +394,18 @@ extern "C" int dgnn_causal_conv_backward(const void *x, const float *taps, const
     if ((dt != DGNN_F32 && dt != DGNN_BF16) || (flags & ~DGNN_SILU)) return DGNN_ERR_SHAPE;
     for (const void *p : {x, x_before, g_y, dx_after, (const void *)dx, (const void *)dx_before, (const void *)ws})
         if (p && !aligned16(p)) return DGNN_ERR_ALIGN;
+    if (!words_aligned({taps, bias, lengths, dtaps, dbias})) return DGNN_ERR_ALIGN;
     size_t need = 0;
     dgnn_causal_conv_backward_workspace(T, n, f, w, &need);
     if (ws_bytes < need) return DGNN_ERR_CAPACITY;
     const size_t row = (size_t)n * f * (dt == DGNN_F32 ? 4 : 2), all = row * T, edge = row * (w - 1);
-    const std::pair<const void *, size_t> in[] = {{x, all}, {x_before, edge}, {g_y, all}, {dx_after, edge}}, out[] = {{dx, all}, {dx_before, edge}, {ws, ws_bytes}};
-    for (int i = 0; i < 3; ++i) {
+    const size_t parameters = sizeof(float) * w * f, vector = sizeof(float) * f;
+    const std::pair<const void *, size_t> in[] = {{x, all}, {x_before, edge}, {g_y, all}, {dx_after, edge}, {taps, parameters}, {bias, vector}, {lengths, sizeof(int32_t) * n}};
+    const std::pair<const void *, size_t> out[] = {{dx, all}, {dx_before, edge}, {ws, ws_bytes}, {dtaps, parameters}, {dbias, vector}};
+    for (size_t i = 0; i < sizeof(out) / sizeof(*out); ++i) {
         for (auto o : in)
             if (overlap(out[i].first, out[i].second, o.first, o.second)) return DGNN_ERR_ALIAS;
-        for (int k = 0; k < i; ++k)
+        for (size_t k = 0; k < i; ++k)
             if (overlap(out[i].first, out[i].second, out[k].first, out[k].second)) return DGNN_ERR_ALIAS;
     }
     ConvBack b{};

@@ -1054,6 +1054,13 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return p && q && p < q + nb && q < p + na;
 }
 
+// Parameters, their gradients and lengths: 32-bit numbers at any address that those may have.
+bool words_aligned(std::initializer_list<const void *> words) {
+    for (const void *p : words)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
+}
+
 }  // namespace
 
 extern "C" int dgnn_selective_scan_checkpoints(int64_t T, int64_t n, int32_t f, int32_t states, size_t *bytes) {
@@ -1078,10 +1085,12 @@ extern "C" int dgnn_selective_scan(const void *x, const void *delta, const void 
     if (dt != DGNN_F32 && dt != DGNN_BF16) return DGNN_ERR_SHAPE;
     for (const void *p : {x, delta, bc, z, (const void *)h_before, (const void *)y, (const void *)h_after, (const void *)checkpoints, (const void *)ws})
         if (p && !aligned16(p)) return DGNN_ERR_ALIGN;
+    if (!words_aligned({a, d, dt_bias, lengths})) return DGNN_ERR_ALIGN;
+    const size_t vector = sizeof(float) * f, ends = sizeof(int32_t) * n;
     const size_t frame = (size_t)T * n * f * (dt == DGNN_F32 ? 4 : 2), rows = (size_t)T * n * 2 * states * (dt == DGNN_F32 ? 4 : 2);
     const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kHeld - 1) / kHeld) * state;
     for (auto o : {std::pair<const void *, size_t>{y, frame}, {h_after, state}, {checkpoints, kept}, {ws, ws_bytes}}) {
-        for (auto i : {std::pair<const void *, size_t>{x, frame}, {delta, frame}, {bc, rows}, {z, frame}})
+        for (auto i : {std::pair<const void *, size_t>{x, frame}, {delta, frame}, {bc, rows}, {z, frame}, {a, vector * states}, {d, vector}, {dt_bias, vector}, {lengths, ends}})
             if (overlap(o.first, o.second, i.first, i.second)) return DGNN_ERR_ALIAS;
         if (!(o.first == h_after && h_after == h_before) && overlap(o.first, o.second, h_before, state)) return DGNN_ERR_ALIAS;
     }
@@ -1140,13 +1149,17 @@ extern "C" int dgnn_selective_scan_backward(const void *x, const void *delta, co
     for (const void *p : {x, delta, bc, z, (const void *)checkpoints, g_y, (const void *)dh_after, (const void *)dx, (const void *)ddelta, (const void *)dbc, (const void *)dz,
                           (const void *)dh_before, (const void *)ws})
         if (p && !aligned16(p)) return DGNN_ERR_ALIGN;
+    if (!words_aligned({a, d, dt_bias, lengths, da, dd, ddt_bias})) return DGNN_ERR_ALIGN;
     size_t need = 0;
     dgnn_selective_scan_backward_workspace(T, n, f, states, &need);
     if (ws_bytes < need) return DGNN_ERR_CAPACITY;
     const size_t frame = (size_t)T * n * f * (dt == DGNN_F32 ? 4 : 2), rows = (size_t)T * n * 2 * states * (dt == DGNN_F32 ? 4 : 2);
     const size_t state = (size_t)n * f * states * sizeof(float), kept = (size_t)((T + kHeld - 1) / kHeld) * state;
-    const std::pair<const void *, size_t> in[] = {{x, frame}, {delta, frame}, {bc, rows}, {z, frame}, {checkpoints, kept}, {g_y, frame}, {dh_after, state}};
-    const std::pair<const void *, size_t> out[] = {{dx, frame}, {ddelta, frame}, {dbc, rows}, {dz, frame}, {dh_before, state}, {ws, ws_bytes}};
+    const size_t vector = sizeof(float) * f;
+    const std::pair<const void *, size_t> in[] = {{x, frame}, {delta, frame}, {bc, rows}, {z, frame}, {checkpoints, kept}, {g_y, frame}, {dh_after, state},
+                                                  {a, vector * states}, {d, vector}, {dt_bias, vector}, {lengths, sizeof(int32_t) * n}};
+    const std::pair<const void *, size_t> out[] = {{dx, frame}, {ddelta, frame}, {dbc, rows}, {dz, frame}, {dh_before, state}, {ws, ws_bytes},
+                                                   {da, vector * states}, {dd, vector}, {ddt_bias, vector}};
     for (size_t i = 0; i < sizeof(out) / sizeof(*out); ++i) {
         for (auto o : in)
             if (overlap(out[i].first, out[i].second, o.first, o.second)) return DGNN_ERR_ALIAS;

@@ -178,3 +178,39 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         dg.Gradients([torch.zeros(3)])
     assert binding.selective_scan_checkpoints(17, 2, 16, 8) == 3 * 2 * 16 * 8
+
+
+def test_parameters_are_inputs_too(lib):
+    """Outputs and workspaces that lie over parameters or lengths, gradients of parameters over anything; 32-bit numbers between two of them."""
+    conv = dict(x=AT[0], taps=AT[1], bias=AT[2], x_before=AT[3], y=AT[4], x_after=AT[5], lengths=AT[6], T=4, n=8, f=32, w=4, flags=8, dt=0)
+    need = size(lib.dgnn_causal_conv_backward_workspace, 4, 8, 32, 4)[1]
+    conv_back = dict(x=AT[0], taps=AT[1], bias=AT[2], x_before=AT[3], g_y=AT[4], dx_after=AT[5], dx=AT[6], dx_before=AT[7], dtaps=AT[8], dbias=AT[9], lengths=AT[11],
+                     T=4, n=8, f=32, w=4, flags=8, accumulate=0, dt=0, ws=AT[10], wsb=need)
+    need = size(lib.dgnn_selective_scan_workspace, 40, 8, 32, 16)[1]
+    scan = dict(x=AT[0], delta=AT[1], bc=AT[2], z=AT[3], a=AT[4], d=AT[5], dt_bias=AT[6], h_before=AT[7], y=AT[8], h_after=AT[9], checkpoints=AT[10], lengths=AT[12],
+                T=40, n=8, f=32, states=16, dt=0, ws=AT[11], wsb=need)
+    need = size(lib.dgnn_selective_scan_backward_workspace, 40, 8, 32, 16)[1]
+    scan_back = dict(x=AT[0], delta=AT[1], bc=AT[2], z=AT[3], a=AT[4], d=AT[5], dt_bias=AT[6], checkpoints=AT[7], g_y=AT[8], dh_after=AT[9], dx=AT[10], ddelta=AT[11],
+                     dbc=AT[12], dz=AT[13], da=AT[14], dd=AT[15], ddt_bias=AT[16], dh_before=AT[17], lengths=AT[19], T=40, n=8, f=32, states=16, accumulate=0, dt=0,
+                     ws=AT[18], wsb=need)
+    vector = 32 * 4
+    sizes = dict(taps=4 * vector, dtaps=4 * vector, a=16 * vector, da=16 * vector, lengths=8 * 4)         # of the others: one number per channel
+    for fn, ok, parameters, gradients, outputs in (
+            (lib.dgnn_causal_conv, conv, ("taps", "bias"), (), ("y", "x_after")),
+            (lib.dgnn_causal_conv_backward, conv_back, ("taps", "bias"), ("dtaps", "dbias"), ("dx", "dx_before", "ws")),
+            (lib.dgnn_selective_scan, scan, ("a", "d", "dt_bias"), (), ("y", "h_after", "checkpoints", "ws")),
+            (lib.dgnn_selective_scan_backward, scan_back, ("a", "d", "dt_bias"), ("da", "dd", "ddt_bias"), ("dx", "ddelta", "dbc", "dz", "dh_before", "ws"))):
+        def call(**kw):
+            return fn(*dict(ok, **kw).values(), None)
+
+        for k in parameters + gradients + ("lengths",):
+            for at in (ok[k] + 1, ok[k] + 2):
+                assert call(**{k: at}) == ALIGN, (fn, k)
+        for o in outputs:
+            for k in parameters + ("lengths",):
+                last = sizes.get(k, vector) - 16                  # 16 bytes inside of it, from either end
+                assert call(**{o: ok[k]}) == ALIAS and call(**{o: ok[k] + last}) == ALIAS, (fn, o, k)
+        inputs = [k for k in ok if k not in gradients + outputs and isinstance(ok[k], int) and ok[k] in AT]
+        for k in gradients:
+            for o in inputs + [o for o in outputs + gradients if o != k]:
+                assert call(**{k: ok[o]}) == ALIAS and call(**{k: ok[o] - sizes.get(k, vector) + 4}) == ALIAS, (fn, k, o)
