@@ -545,3 +545,38 @@ def test_scan_all_states_forgotten():
     got = s.backward(kept)
     assert not y.any() and torch.equal(after.cpu(), s.h_before) and torch.equal(got["dh_before"].cpu(), s.dh_after)
     assert not any(got[k].any() for k in got if k != "dh_before")
+
+
+def carried(step, a):
+    """How many timesteps' roundings a state carries with it, at most.  k timesteps' stay with a term that has decayed by exp(-u), u = the sum of step
+    size times |a| over them, and M holds exp(-7/8 u) of it: k exp(-u / 8) of M.  The largest over all stretches of the series, from
+    those of 1, 2, 4, ... timesteps: one of up to 2 k contains one of k."""
+    slowest = np.abs(a).min(1)[None, None, :]
+    total = np.concatenate([np.zeros((1,) + step.shape[1:]), np.cumsum(step, 0)])
+    most, k = 2.0, 1
+    while k < len(total):
+        least = (total[k:] - total[:-k]) * slowest
+        most = max(most, float((2 * k * np.exp(-least.min(0) / 8)).max()))
+        k *= 2
+    return min(most, len(step))
+
+
+@pytest.mark.parametrize("T,n,f,N", [(70_001, 1, 16, 8), (9000, 2, 16, 32), (20_000, 1, 32, 16)])
+def test_scan_long_as_its_states_last(T, n, f, N):
+    """Hundreds of pieces against a bound that goes by how long a state lasts and not by how long the series is.  Ahead of it as above, 64 and 65, and
+    what pieces add: the decay across one has its step sizes added up (a lane's, up to 36 of them here; in a run of pieces 16 more and 5 over
+    the runs, roundings of a positive sum all of them) and its product taken once more, 60 2^-24 of its exponent: 60 8 / e = 177 more."""
+    s = Scan(T, n, f, N, F32, seed=T)
+    a = s.oracle()
+    depth = 64 + 65 + 177 + 4 * carried(tp.softplus(a["delta"] + a["dt_bias"]), a["a"])
+    assert depth < 129 + T                                        # four times as close as by the series' length, at least
+    y, after, kept = s.forward()
+    want, want_after, _ = tp.selective_scan(**a)
+    mag, mag_after, _ = tp.selective_scan(magnitudes=True, **a)
+    close(y, want, mag, depth, "y")
+    close(after, want_after, mag_after, depth, "h_after")
+    got = s.backward(kept)
+    h = dict(a, g_y=np64(s.g_y), dh_after=np64(s.dh_after))
+    want, mag = tp.selective_scan_backward(**h), tp.selective_scan_backward(magnitudes=True, **h)
+    for k in ("dx", "ddelta", "dbc", "dz", "dh_before"):
+        close(got[k], want[k], mag[k], 2 * depth + f, k)          # a state and a gradient that were carried meet
