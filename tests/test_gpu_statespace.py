@@ -371,3 +371,47 @@ def test_a_refused_forward_leaves_nothing_to_go_back_through():
         layer.backward(x)
     layer.forward(x, train=True)
     layer.backward(x)
+
+
+def rounded_layer(p, x, g_out):
+    """The layer in 64 bits with every tensor between its steps rounded to bf16, as it is stored: outputs, dL/dx, gradients."""
+    r = lambda v: torch.from_numpy(np.ascontiguousarray(v)).bfloat16().double().numpy()  # noqa: E731
+    rows = lambda a, b: a.reshape(-1, a.shape[-1]).T @ b.reshape(-1, b.shape[-1])  # noqa: E731
+    q = {k: np64(v) for k, v in p.items()}
+    x, g_out = np64(x), np64(g_out)
+    u0, z = r(x @ q["w_in"]), r(x @ q["w_z"])
+    conv = dict(taps=q["taps"], bias=q["conv_bias"], act=True)
+    u = r(tp.causal_conv(u0, **conv)[0])
+    scan = dict(x=u, delta=r(u @ q["w_dt"]), bc=r(u @ q["w_bc"]), a=q["a"], z=z, d=q["d"], dt_bias=q["dt_bias"])
+    y = r(tp.selective_scan(**scan)[0])
+    g = tp.selective_scan_backward(g_y=r(g_out @ q["w_out"].T), **scan)
+    du = r(g["dx"])
+    for k, name in (("ddelta", "w_dt"), ("dbc", "w_bc")):
+        g[k] = r(g[k])
+        du = r(du + r(g[k] @ q[name].T))
+    g["dz"] = r(g["dz"])
+    c = tp.causal_conv_backward(u0, g_y=du, **conv)
+    c["dx"] = r(c["dx"])
+    grads = dict(w_out=rows(y, g_out), w_dt=rows(u, g["ddelta"]), w_bc=rows(u, g["dbc"]), w_in=rows(x, c["dx"]), w_z=rows(x, g["dz"]), taps=c["dtaps"],
+                 conv_bias=c["dbias"], a=g["da"], d=g["dd"], dt_bias=g["ddt_bias"])
+    return r(y @ q["w_out"]), r(r(c["dx"] @ q["w_in"].T) + r(g["dz"] @ q["w_z"].T)), grads
+
+
+@pytest.mark.parametrize("T,n,f,d,states,w", [(18, 64, 32, 64, 16, 4), (7, 90, 64, 128, 32, 3), (41, 20, 16, 16, 8, 2)])
+def test_bf16_layer(T, n, f, d, states, w):
+    """bf16 frames against 64 bits that round where the layer stores.  What is left are values so near to the middle of two bf16 numbers that the
+    layer's fp32 sums, off by some 2^-22 of the magnitudes that meet in them (four times the result), fall on the other side: 2^-22 4 2 / 2^-8 =
+    2^-11 of all values, off by a step of at most 2^-7 of the value, which is sqrt(2^-11) 2^-7 = 2^-12.5 of a tensor's norm.  Twelve tensors
+    are rounded one after the other, each error grows by four at most until the end (sums whose terms cancel): sqrt(12) 4 2^-12.5 < 2^-8 of
+    a result's norm, and twice that here; single entries, of which a step of their own is 2^-7, 2^-4 of the largest."""
+    p = make_weights(f, d, states, w, dtype=torch.bfloat16)
+    g = torch.Generator().manual_seed(T)
+    x, g_out = torch.randn((T, n, f), generator=g).to(DEV).bfloat16(), torch.randn((T, n, f), generator=g).to(DEV).bfloat16()
+    layer = StateSpaceLayer(n, T, p)
+    out = layer.forward(x, train=True).clone()
+    dx = layer.backward(g_out)
+    want, want_dx, grads = rounded_layer(p, x, g_out)
+    near(out, want, "out", 2.0 ** -7, 2.0 ** -4)
+    near(dx, want_dx, "dx", 2.0 ** -7, 2.0 ** -4)
+    for k in WEIGHTS + PARAMETERS:
+        near(layer.grads[k], grads[k], k, 2.0 ** -7, 2.0 ** -4)
