@@ -729,7 +729,7 @@ int dgnn_causal_conv_backward(const void *x, const float *taps, const float *bia
  *   checkpoints                  NULL, or fp32 of dgnn_selective_scan_checkpoints() bytes: the state ahead of every 8th timestep,
  *                                which is what the adjoint needs of the forward pass
  *   ws                           dgnn_selective_scan_workspace() bytes, 16-byte aligned
- * States, step sizes and sums are fp32, y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose
+ * States, step sizes and sums are fp32 (a decay below 2^-126 is zero), y is rounded once.  Few sequences of many timesteps are cut into pieces of the time axis whose
  * states are joined afterwards: the same sums in another order.  Results repeat bit for bit.
  * Errors: NULL, SHAPE, OVERFLOW (T beyond 2^30, T * n beyond 2^44 too), ALIGN, ALIAS (as above; the workspace is an output), CAPACITY.
  */

@@ -8,6 +8,7 @@
 // of the second pass adds up the workgroups' sums by itself, in one fixed order, instead of waiting for a launch that does, while its first
 // stretch is on its way.  Bound by memory: 400 M elements in nine tensors of both types (1.33 GB) take 743 us, 3.6 TB/s of one read and one
 // write, 5.4 with the second read, which the norm cannot do without (240 us the squares, 485 the scaling); 46 tensors of 90 K elements 4 + 5 us.
+// In place under the bound, where nothing is scaled, the second pass still reads: 432 us, of which the norm is 221.
 #include <algorithm>
 #include <vector>
 

@@ -32,11 +32,11 @@ constexpr int kChannels = 16;             // channels of a wavefront
 constexpr int kTile = 16;                 // timesteps of a tile, but for short series
 constexpr int kPiece = 16;                // ... of a piece of the time axis, at least; pieces are multiples of it
 // ... between two kept states: the adjoint holds the states of so many timesteps in registers (sixteen would be 32 registers more with 16 states,
-// which spill); the forward pass writes 4 N / 8 bytes a value for them.
+// beyond the 256 there are); the forward pass writes 4 N / 8 bytes a value for them.
 constexpr int kHeld = 8;
 constexpr int kWaves = 4;                 // wavefronts of a workgroup of the kernels without sums over channels
 // Wavefronts of a workgroup of the adjoint at most, and of all its workgroups: two on a SIMD, and three with 8 states, whose registers
-// allow it (2^17 x 128 fp32: 226 us with two, 193 with three); workgroups of four then, for three times eight do not fit.
+// allow it (16 x 8192 x 128 fp32: 225 us with two, 187 with three); workgroups of four then, for three times eight do not fit.
 constexpr int back_waves(int states) { return states == 8 ? 4 : 8; }
 constexpr int back_resident(int states) { return (states == 8 ? 3 : 2) * 4 * 256; }   // of 4 SIMDs on 256 CUs
 constexpr int kMaxGrid = 1 << 22;         // workgroups of a launch: HIP counts its threads in 32 bits
@@ -68,7 +68,7 @@ struct ScanBack {
 };
 
 // ---- arithmetic ---------------------------------------------------------------------------------------------------
-// 2^x and 1 / x by the hardware's instructions, 1 unit in the last place each.
+// 2^x and 1 / x by the hardware's instructions, 1 unit in the last place each; 2^x is zero below 2^-126, and so are decays.
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float rcp_of(float x) { return __builtin_amdgcn_rcpf(x); }
 
@@ -80,7 +80,8 @@ __device__ __forceinline__ float exp_of(float v) {
 }
 
 // softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|), and sig(v).  log(1 + e) = 2 artanh(r) with r = e / (2 + e) <= 1/3, an odd series:
-// r P(r^2) with the polynomial of degree 4 that meets it at the Chebyshev nodes of [0, 1/9], 4e-9 of the result off.  A small e loses no
+// r P(r^2) with the polynomial of degree 4 that meets it at the Chebyshev nodes of [0, 1/9], 8e-9 of the result off (an eighth of fp32's half
+// step) with its coefficients rounded to fp32.  A small e loses no
 // digits, which 1 + e would.
 __device__ __forceinline__ float softplus_of(float v, float &sig) {
     const float e = exp_of(-fabsf(v));
@@ -283,8 +284,8 @@ template <bool BF16, int S, int K> struct Rows {
 // ---- forward ------------------------------------------------------------------------------------------------------
 // What bounds it: vector instructions, then memory.  A state takes five a timestep (two products, the exponential, which holds the pipe for
 // two, two multiply-adds), a lane's four 24 slots of some 34; the rest is the step sizes (25 instructions for four timesteps), the exchange of
-// four timesteps' sums (9), the gate, addresses.  16 x 100003 x 64 fp32, 16 states, gated: 568 us, vector instructions in 81 % of the cycles at
-// five wavefronts per SIMD, 4.0 TB/s of the 4.8 that a copy reaches; bf16 at half the bytes takes the same.
+// four timesteps' sums (9), the gate, addresses.  16 x 100003 x 64 fp32, 16 states, gated: 571 - 583 us, vector instructions in 81 % of the cycles at
+// five wavefronts per SIMD, 3.9 TB/s of the 4.5 - 5.4 that copies reach; bf16 at half the bytes, bound by instructions alone, 509.
 template <bool BF16, int S, int K> struct Tile {
     Rows<BF16, S, K> rows;
     float x[K / 4], delta[K / 4], z[K / 4], h[S];
@@ -639,12 +640,14 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_back_piece_kernel(ScanBack
     }
 }
 
-// Timesteps of a tile of the adjoint at most: what a wavefront fetches ahead.  Sixteen where the registers hold them (64 sequences of 1024 x 128 bf16: 181 us
-// against 189 with eight; with 8 states, at three wavefronts per SIMD, 188 with eight and 200 with sixteen; with 32 they spill).
+// Timesteps of a tile of the adjoint at most: what a wavefront fetches ahead.  Sixteen with 16 states (256 x 512 x 128 bf16: 268 us against 294 with eight;
+// 16 x 8192 x 128 fp32 276 against 271); with 8 states, at three wavefronts per SIMD, eight (187 against 216).  With 32 the registers are short with
+// eight already: all 256 are in use and 38 - 60 values a lane go through scratch memory; with sixteen it is 180 - 268 (16 x 4096 x 128 fp32: 281 us
+// against 929).
 template <int S> constexpr int kBackTile = S == 4 ? 16 : 8;
 // Whether a tile's loads are all made, whatever is there of it.  With 32 states, where the registers are short, the loads that a branch may
-// pass over cost more (2^17 x 128 fp32: 922 us against 658), and with 16 in bf16 (256 x 512 x 128: 303 against 272); with 16 in fp32 the
-// addresses that take the branches' place do where half of a tile is there (7 x 20000 x 64: 230 against 209; 16 x 8192 x 128: 281 against 278), and with 8 neither.
+// pass over cost more (16 x 8192 x 128 fp32: 859 us against 556), and with 16 in bf16 (256 x 512 x 128: 299 against 268); with 16 in fp32 and with
+// 8 it makes no difference in whole tiles (16 x 8192 x 128: 276 and 280; 7 x 20000 x 64: 186 and 187; 8 states 187 and 185), and nothing is loaded that is not there.
 template <bool BF16, int S> constexpr bool kAllLoads = S > 4 || (BF16 && S == 4);
 
 template <bool BF16, int S, int K> struct BackTile {
@@ -691,14 +694,14 @@ __device__ __forceinline__ void load_back_tile(BackTile<BF16, S, K> &r, const Sc
 // (five instructions a state and timestep) and back again (eight, and 4 for the sums over channels): some 108 a timestep and lane with 16
 // states, and they are what bounds it: 16 x 50021 x 32 fp32 takes 425 us with vector instructions in 80 % of the cycles at two wavefronts per SIMD, 2.9
 // TB/s with the forward pass.  The exchange over channels is 16 of them, its cost when left out 19 %; the matrix cores would take the sums at the same number of
-// issue slots.  16 x 8192 x 128 fp32: 188 us with 8 states, 279 with 16; 16 x 4096 x 128 with 32: 289, bf16 267.
+// issue slots.  16 x 8192 x 128 fp32: 187 us with 8 states, 276 with 16; 16 x 4096 x 128 with 32 (which spill): 281, bf16 276.
 template <bool BF16, int S, bool GATE, int K>
 __global__ __launch_bounds__(back_waves(4 * S) * kWave) void scan_back_kernel(ScanBack b) {
     typedef typename Elem<BF16>::Type E;
     constexpr int N = 4 * S, R = K / 4, V = K * 2 * N;  // V: values of dB and dC of a tile
     constexpr int J = S <= 4 ? 4 : 2;                                     // timesteps whose sums over channels are exchanged together
-    // With 32 states in fp32 what two fours have in flight together does not fit the registers: they stay apart (16 x 4096 x 128: 291 us against 334);
-    // in bf16 it does (253 against 277).
+    // With 32 states in fp32 what two fours have in flight together does not fit the registers: they stay apart (16 x 4096 x 128: 281 us against 294);
+    // in bf16 they do not (276 against 289).
     constexpr bool kFence = S > 4 && !BF16;
     // [3][wavefronts][V], the three by turns: B and C of a tile, where dB and dC take their place timestep by timestep (the next tile's B
     // and C are laid down when a slower wavefront may still be adding up this one's dB and dC); 64-bit sums.  Decays are formed twice: kept here

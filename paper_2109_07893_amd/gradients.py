@@ -56,7 +56,8 @@ class Gradients:
         return self.scalar
 
     def clip(self, max_norm: float) -> torch.Tensor:
-        """out = g min(1, max_norm / (norm + 1e-6)); returns the norm from before.  A norm that is no finite number changes nothing."""
+        """out = g min(1, max_norm / (norm + 1e-6)); returns the norm from before, the same scalar as norm().  A norm that is no finite number
+        changes nothing."""
         B.grad_clip(len(self.grads), self.table.at(), max_norm, self.result, self.ws)
         return self.scalar
 
@@ -72,7 +73,7 @@ class ClipsGradients:
 
     def clip_gradients(self, max_norm: float) -> torch.Tensor:
         """Scales them, where they lie, so that the norm over all of them is at most max_norm; returns the norm from before, a scalar on
-        the device.  A norm that is no finite number changes nothing."""
+        the device that the next call overwrites.  A norm that is no finite number changes nothing."""
         grads = self.parameter_gradients()
         bound = self._clipped
         if bound is None or len(bound.grads) != len(grads) or any(a is not b for a, b in zip(bound.grads, grads)):
